@@ -515,6 +515,75 @@ int mpc_maxpool2x2_backward(mpc_ctx* ctx, mpc_cshare g, mpc_cshare s1, mpc_cshar
                             mpc_cshare a2, mpc_cshare b2, mpc_cshare c2,
                             mpc_share gx, int B, int H, int W, int C);
 
+/* ------------------------- attention without a softmax, public 4-bit weights */
+
+/* The encoder layer's attention is linear here: scores feed the second product directly (Sec. 5.3's products, the softmax
+ * left out).  The calls below give it positions, a form whose cost grows with the length instead of its square and that
+ * serves single tokens, and projections by public weights.  They run on the lane's first stream, on every lane, and their
+ * exchanges are remote stores whatever mpc_ctx_set_exchange says.  Outputs may not overlap an input other than where it is
+ * said (MPC_EINVAL). */
+
+/* Learned relative position bias.  scores, out: [B][H][Tq][Tk]; table: [n_buckets][H]; buckets: public int32
+ * [Tq + Tk - 1] on the device, entry j - i + Tq - 1 is the bucket of query i and key j.
+ *   out[b][h][i][j] = scores[b][h][i][j] + table[bucket][h]
+ * An entry outside [0, n_buckets) masks its pairs: out is a sharing of zero there (both words zero).  Local: no triple, no
+ * exchange.  out may be scores itself.  No workspace.
+ * mpc_position_bias_grad: table_grad[u][h] = sum of g[b][h][i][j] over b and all pairs of bucket u (written, not added to);
+ * scores_grad (both NULL to skip; may be g itself) = g, zero at masked pairs.  Sums mod 2^64 are exact: the result does not
+ * depend on their order.
+ * MPC_ERANGE: n_buckets > MPC_MAX_BUCKETS, or sizes beyond 2^31. */
+#define MPC_MAX_BUCKETS 4096
+int mpc_position_bias(mpc_ctx* ctx, mpc_cshare scores, mpc_cshare table, const int32_t* buckets, mpc_share out,
+                      int B, int H, int Tq, int Tk, int n_buckets);
+int mpc_position_bias_grad(mpc_ctx* ctx, mpc_cshare g, const int32_t* buckets, mpc_share table_grad, mpc_share scores_grad,
+                           int B, int H, int Tq, int Tk, int n_buckets);
+
+/* z = x * w^T with public weights in 4 bits: w[n][k] = q[n][k] * scales[n][k / group], q in [-8, 7].  x: [M][K], z: [M][N].
+ * w: rows of 16 * ceil(K / 32) bytes, 16-byte aligned; byte k / 2 of a row holds q[n][k] of an even k in its low half, of an
+ * odd k in its high half, in two's complement (what lies behind column K is not used).  scales: int32
+ * [N][ceil(K / group)] with scale_bits fraction bits in [0, 31]; the product is rescaled by them (the local truncation of
+ * mpc_truncate), so z has the fixed point of x.  group: 32, 64 or a multiple of 128.  Linear in the shares with public
+ * factors, so each party works alone: no triple, no exchange.  No workspace.  A call reads the weights once for every eight
+ * rows of x.  MPC_ERANGE: K > MPC_MAX_K_TOTAL, M > 65535. */
+int mpc_matvec4(mpc_ctx* ctx, mpc_cshare x, const uint8_t* w, const int32_t* scales, mpc_share z,
+                int M, int K, int N, int group, int scale_bits);
+
+/* Linear attention with a public decay g for each head: S_t = g S_(t-1) + k_t v_t^T (dk x dv), o_t = q_t S_t.
+ *
+ * Where the words of q, k, v, o lie: word e of (batch b, token t, head h) at b*batch + t*token + h*head + e, strides in
+ * words, both shares alike; any non-negative strides for inputs, outputs without words that share a place.
+ * decay: int32 [H][65] on the device, public: entry n of a head is rint(g^n * 2^frac_bits); every entry in [0, 2^31).
+ * Everything else is dense.
+ *
+ * mpc_linear_attention: T tokens, in chunks of 64 (L in the last one).  trunc is the local rescale by frac_bits:
+ *   P = trunc(Q K^T)   W[i][j] = trunc(P[i][j] g^(i-j)) for j <= i, else 0   Qd[i] = trunc(Q[i] g^(i+1))
+ *   Kd[j] = trunc(K[j] g^(L-1-j))   U = Kd^T V   S' = trunc(g^L S + U)   O = trunc([W | Qd] [V ; S])
+ * with S the state before the chunk.  state: [B][H][dk][dv] before the first token, both NULL for zero; state_out: after the
+ * last one, both NULL to skip; it may be state itself.
+ * mpc_linear_attention_step: one token, S' = trunc(g S + k v^T), o = trunc(q S').  state and state_out are required.
+ *
+ * Material, masks a_* and addends c_*, uniform words like every triple; BH = B * H.  Party 0's addend has its local product
+ * taken off (as mpc_matmul_fold does): c_0 + c_1 = products below - (party 0's own products).
+ *   prompt: a_q, a_k, a_qd, a_kd [BH][T][dk] (masks of Q, K, Qd, Kd); a_v [BH][T][dv]; a_w [BH][T][64] (row of a token,
+ *     column of the chunk's token; above the diagonal nothing is read, and a_w counts as zero in c_o);
+ *     a_s [BH][chunks][dk][dv] (mask of the state before each chunk);
+ *     c_p [BH][T][64] of a_q a_k^T, c_u [BH][chunks][dk][dv] of a_kd^T a_v, c_o [BH][T][dv] of a_w a_v + a_qd a_s
+ *   step: a_q, a_k [BH][dk], a_v [BH][dv], a_s [BH][dk][dv] (mask of S'); c_u [BH][dk][dv] of a_k a_v^T, c_o [BH][dv] of a_q a_s
+ * MPC_ERANGE: dk or dv beyond MPC_ATTENTION_MAX_D, frac_bits > 30, B * H beyond 2^31.  Workspace: the queries. */
+#define MPC_ATTENTION_CHUNK 64
+#define MPC_ATTENTION_MAX_D 128
+typedef struct { int64_t batch, token, head; } mpc_strides;
+typedef struct { mpc_cshare a_q, a_k, a_qd, a_kd, a_v, a_w, a_s, c_p, c_u, c_o; } mpc_attention_material;
+typedef struct { mpc_cshare a_q, a_k, a_v, a_s, c_u, c_o; } mpc_attention_step_material;
+size_t mpc_linear_attention_workspace_bytes(int B, int T, int H, int dk, int dv);
+int mpc_linear_attention(mpc_ctx* ctx, mpc_cshare q, mpc_cshare k, mpc_cshare v, mpc_strides sq, mpc_strides sk, mpc_strides sv,
+                         const int32_t* decay, const mpc_attention_material* mat, mpc_cshare state, mpc_share o, mpc_strides so,
+                         mpc_share state_out, int B, int T, int H, int dk, int dv);
+size_t mpc_linear_attention_step_workspace_bytes(int B, int H, int dk, int dv);
+int mpc_linear_attention_step(mpc_ctx* ctx, mpc_cshare q, mpc_cshare k, mpc_cshare v, mpc_strides sq, mpc_strides sk, mpc_strides sv,
+                              const int32_t* decay, const mpc_attention_step_material* mat, mpc_cshare state, mpc_share o,
+                              mpc_strides so, mpc_share state_out, int B, int H, int dk, int dv);
+
 /* ------------------------------------------ three parties (Sec. 3.3, Sec. 5.6) */
 
 /* Alg. 1 and Alg. 2 are stated for N parties.  The calls below run them for

@@ -1,0 +1,478 @@
+// Linear attention with a public decay for each head, on shares: S_t = g S_{t-1} + k_t v_t^T, o_t = q_t S_t.
+//
+// One token (mpc_linear_attention_step): U = k v^T and q S are Beaver products, the decay is a public factor that joins U at
+// scale 2^2f so that one rescale serves both: S' = trunc(g S + U), o = trunc(q S').
+//
+// Prompts (mpc_linear_attention), in chunks of 64 tokens, pow[n] = g^n, L tokens in the chunk:
+//   P = trunc(Q K^T), W[i][j] = trunc(P[i][j] pow[i-j]) for j <= i, else zero    Qd[i] = trunc(Q[i] pow[i+1])
+//   Kd[j] = trunc(K[j] pow[L-1-j]), U = Kd^T V                                   S' = trunc(pow[L] S + U)
+//   O = trunc([W | Qd] [V ; S])
+// Three launches: everything that one chunk has for itself (P, W, U and their openings), the states from chunk to chunk
+// (element by element), and O of all chunks.
+//
+// All products are Alg. 1 with party 0's local product folded into its addend (the folded calls of the linear layers):
+// party 0 has c_0 + (x_0 + e_1)(y_0 + f_1), party 1 has c_1 + e b_1 + a_1 f.  The exchange is by remote store: a masked word is
+// stored into the peer's receive buffer and used as it passes.
+#include "attention.h"
+
+namespace {
+
+constexpr int kChunk = MPC_ATTENTION_CHUNK;   // 64
+constexpr int kThreads = 512;
+constexpr int kUnit = 16;                     // words along the contraction that a thread brings
+constexpr int kBoxes = 512;                   // workgroups of a launch, each with receive buffers of its own
+constexpr size_t kBoxWords = (size_t)kThreads * kUnit;   // per direction
+
+struct Rows { const u64* p[2]; long long b, t, h; };     // words of (batch, token, head) at p + b*b + t*t + h*h
+
+struct ChunkArgs {
+    Rows q, k, v;
+    const u64 *a_q[2], *a_k[2], *a_qd[2], *a_kd[2], *a_v[2], *a_w[2], *a_s[2], *c_p[2], *c_u[2], *c_o[2], *state[2];
+    u64 *o[2]; long long ob, ot, oh;
+    u64* state_out[2];
+    const int32_t* decay;                     // [H][65]
+    u64* recv_v[2];                           // what the peer sent of V: [BH][T][dv]
+    u64 *w_x0, *w_open;                       // W: party 0's operand, opened words: [BH][T][64]
+    u64* u[2];                                // U; then the states: party 0's operand (u[0]) and opened words (u[1]): [BH][chunks][dk][dv]
+    u64* box;
+    int B, H, T, dk, dv, chunks, bits;
+    int mt, nt;                               // tiles of 64 along dk and dv
+};
+
+// The words of a thread's unit: 16 along the contraction of one row.
+struct Unit { u64 own0[kUnit], open[kUnit], mask1[kUnit]; };   // party 0's operand x_0 + e_1; e; a_1
+
+// A masked operand: x, a of both parties at offset k*kx / k*ka from a row's first word; n of the 16 words are there.
+// power(k): public factor and rescale before masking, or none.
+template <bool DECAY, class Power>
+__device__ __forceinline__ void open_unit(Unit& u, const u64* x0, const u64* x1, long long kx, const u64* a0, const u64* a1, long long ka,
+                                          int n, Power power, int bits, u64* to0, u64* to1, long long kt)
+{
+#pragma unroll
+    for (int k = 0; k < kUnit; ++k) {
+        u.own0[k] = u.open[k] = u.mask1[k] = 0;
+        if (k >= n) continue;
+        u64 w0 = x0[k * kx], w1 = x1[k * kx];
+        if (DECAY) { const u64 f = power(k); w0 = rescaled<0>(w0 * f, bits); w1 = rescaled<1>(w1 * f, bits); }
+        const u64 m1 = a1[k * ka], e0 = w0 - a0[k * ka], e1 = w1 - m1;
+        if (to0) { to0[k * kt] = e1; to1[k * kt] = e0; }      // the exchange
+        u.own0[k] = w0 + e1; u.open[k] = e1 + e0; u.mask1[k] = m1;
+    }
+}
+
+// ---- products of 64 x 64 x 64 words: tile words in LDS, left [k][row], right [k][col]
+struct Tile { u64 left[64][64], right[64][64]; };
+
+__device__ __forceinline__ void stage(Tile& s, const u64 (&w)[kUnit])
+{
+    const int t = threadIdx.x % 256, row = t % 64, kb = t / 64;
+    u64 (*const to)[64] = threadIdx.x < 256 ? s.left : s.right;
+#pragma unroll
+    for (int k = 0; k < kUnit; ++k) to[kb * kUnit + k][row] = w[k];
+}
+__device__ __forceinline__ void multiply(const Tile& s, u64 (&z)[8])
+{
+    const int col = threadIdx.x % 64, r0 = threadIdx.x / 64 * 8;
+    for (int k = 0; k < 64; ++k) {
+        const u64 y = s.right[k][col];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) z[r] += s.left[k][r0 + r] * y;
+    }
+}
+// z0 += own0 own0', z1 += open mask1' + mask1 open'
+__device__ __forceinline__ void multiply_unit(Tile& s, const Unit& u, u64 (&z0)[8], u64 (&z1)[8])
+{
+    const bool left = threadIdx.x < 256;
+    __syncthreads();
+    stage(s, u.own0);
+    __syncthreads();
+    multiply(s, z0);
+    __syncthreads();
+    if (left) stage(s, u.open); else stage(s, u.mask1);
+    __syncthreads();
+    multiply(s, z1);
+    __syncthreads();
+    if (left) stage(s, u.mask1); else stage(s, u.open);
+    __syncthreads();
+    multiply(s, z1);
+}
+template <class Each> __device__ __forceinline__ void each_word(Each each)
+{
+    const int col = threadIdx.x % 64, r0 = threadIdx.x / 64 * 8;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) each(r, r0 + r, col);
+}
+
+struct NoPower { __device__ u64 operator()(int) const { return 1; } };
+
+// P and W of a chunk, or one tile of its U.
+__global__ __launch_bounds__(kThreads) void k_chunk_open(ChunkArgs q)
+{
+    __shared__ Tile s;
+    const int t = threadIdx.x % 256, row = t % 64, kb = t / 64;
+    const bool left = threadIdx.x < 256;
+    u64* const box0 = q.box + blockIdx.x * 2 * kBoxWords + threadIdx.x;
+    u64* const box1 = box0 + kBoxWords;
+    const long long jobs = (long long)q.B * q.H * q.chunks * (1 + q.mt * q.nt);
+    for (long long job = blockIdx.x; job < jobs; job += gridDim.x) {
+        const int kind = (int)(job % (1 + q.mt * q.nt));
+        const int chunk = (int)(job / (1 + q.mt * q.nt) % q.chunks);
+        const long long bh = job / (1 + q.mt * q.nt) / q.chunks;
+        const int b = (int)(bh / q.H), h = (int)(bh % q.H), t0 = chunk * kChunk, L = q.T - t0 < kChunk ? q.T - t0 : kChunk;
+        const int32_t* const pow = q.decay + h * (kChunk + 1);
+        const long long at = bh * q.T + t0;                       // the chunk's first token in the dense arrays
+        u64 z0[8] = {}, z1[8] = {};
+        if (kind == 0) {
+            const Rows& x = left ? q.q : q.k;
+            const u64* const* a = left ? q.a_q : q.a_k;
+            for (int k0 = 0; k0 < q.dk; k0 += 64) {
+                const int k = k0 + kb * kUnit, n = row < L ? q.dk - k : 0;
+                const long long o = b * x.b + h * x.h + (t0 + row) * x.t + k, oa = (at + row) * q.dk + k;
+                Unit u;
+                open_unit<false>(u, x.p[0] + o, x.p[1] + o, 1, a[0] + oa, a[1] + oa, 1, n, NoPower{}, 0, box0, box1, kThreads);
+                multiply_unit(s, u, z0, z1);
+            }
+            each_word([&](int r, int i, int j) {
+                if (i >= L || j > i) return;
+                const long long o = (at + i) * kChunk + j;
+                const u64 f = (u64)(int64_t)pow[i - j];
+                const u64 w0 = rescaled<0>(rescaled<0>(q.c_p[0][o] + z0[r], q.bits) * f, q.bits);
+                const u64 w1 = rescaled<1>(rescaled<1>(q.c_p[1][o] + z1[r], q.bits) * f, q.bits);
+                const u64 e0 = w0 - q.a_w[0][o], e1 = w1 - q.a_w[1][o];
+                box0[(long long)r * kThreads] = e1; box1[(long long)r * kThreads] = e0;
+                q.w_x0[o] = w0 + e1; q.w_open[o] = e0 + e1;
+            });
+        } else {
+            const int m0 = (kind - 1) / q.nt * 64, n0 = (kind - 1) % q.nt * 64;
+            const int j = kb * kUnit, n = L - j;                  // contraction over the chunk's tokens
+            Unit u;
+            if (left) {
+                const int d = m0 + row;
+                const long long o = b * q.k.b + h * q.k.h + (t0 + j) * q.k.t + d, oa = (at + j) * q.dk + d;
+                open_unit<true>(u, q.k.p[0] + o, q.k.p[1] + o, q.k.t, q.a_kd[0] + oa, q.a_kd[1] + oa, q.dk, d < q.dk ? n : 0,
+                                [&](int k) { return (u64)(int64_t)pow[L - 1 - j - k]; }, q.bits, n0 == 0 ? box0 : nullptr, box1, kThreads);
+            } else {
+                const int d = n0 + row;
+                const long long o = b * q.v.b + h * q.v.h + (t0 + j) * q.v.t + d, oa = (at + j) * q.dv + d;
+                open_unit<false>(u, q.v.p[0] + o, q.v.p[1] + o, q.v.t, q.a_v[0] + oa, q.a_v[1] + oa, q.dv, d < q.dv ? n : 0, NoPower{}, 0,
+                                 m0 == 0 ? q.recv_v[0] + oa : nullptr, q.recv_v[1] + oa, q.dv);
+            }
+            multiply_unit(s, u, z0, z1);
+            each_word([&](int r, int i, int jj) {
+                const int d = m0 + i, e = n0 + jj;
+                if (d >= q.dk || e >= q.dv) return;
+                const long long o = ((bh * q.chunks + chunk) * q.dk + d) * q.dv + e;
+                q.u[0][o] = q.c_u[0][o] + z0[r]; q.u[1][o] = q.c_u[1][o] + z1[r];
+            });
+        }
+    }
+}
+
+// From chunk to chunk, a state element to a thread: what the chunk's O needs of S takes the place of its U.
+__global__ __launch_bounds__(256) void k_chunk_states(ChunkArgs q)
+{
+    const long long per = (long long)q.dk * q.dv, n = (long long)q.B * q.H * per;
+    u64* const box0 = q.box + (size_t)blockIdx.x * 512 + threadIdx.x;
+    for (long long e = (long long)blockIdx.x * 256 + threadIdx.x; e < n; e += (long long)gridDim.x * 256) {
+        const long long bh = e / per, first = bh * q.chunks * per + e % per;
+        const int32_t* const pow = q.decay + bh % q.H * (kChunk + 1);
+        u64 s0 = q.state[0] ? q.state[0][e] : 0, s1 = q.state[0] ? q.state[1][e] : 0;
+        for (int c = 0; c < q.chunks; ++c) {
+            const long long o = first + c * per;
+            const u64 u0 = q.u[0][o], u1 = q.u[1][o], e0 = s0 - q.a_s[0][o], e1 = s1 - q.a_s[1][o];
+            box0[0] = e1; box0[256] = e0;
+            q.u[0][o] = s0 + e1; q.u[1][o] = e0 + e1;
+            const int L = q.T - c * kChunk < kChunk ? q.T - c * kChunk : kChunk;
+            const u64 f = (u64)(int64_t)pow[L];
+            s0 = rescaled<0>(s0 * f + u0, q.bits); s1 = rescaled<1>(s1 * f + u1, q.bits);
+        }
+        if (q.state_out[0]) { q.state_out[0][e] = s0; q.state_out[1][e] = s1; }
+    }
+}
+
+// O of a chunk, 64 columns of dv: first the part within the chunk, then the state's.
+__global__ __launch_bounds__(kThreads) void k_chunk_out(ChunkArgs q)
+{
+    __shared__ Tile s;
+    const int t = threadIdx.x % 256, row = t % 64, kb = t / 64;
+    const bool left = threadIdx.x < 256;
+    u64* const box0 = q.box + blockIdx.x * 2 * kBoxWords + threadIdx.x;
+    u64* const box1 = box0 + kBoxWords;
+    const long long jobs = (long long)q.B * q.H * q.chunks * q.nt;
+    for (long long job = blockIdx.x; job < jobs; job += gridDim.x) {
+        const int n0 = (int)(job % q.nt) * 64, chunk = (int)(job / q.nt % q.chunks);
+        const long long bh = job / q.nt / q.chunks;
+        const int b = (int)(bh / q.H), h = (int)(bh % q.H), t0 = chunk * kChunk, L = q.T - t0 < kChunk ? q.T - t0 : kChunk;
+        const int32_t* const pow = q.decay + h * (kChunk + 1);
+        const long long at = bh * q.T + t0;
+        u64 z0[8] = {}, z1[8] = {};
+        Unit u;
+#pragma unroll
+        for (int k = 0; k < kUnit; ++k) {
+            const int j = kb * kUnit + k, d = n0 + row;
+            u.own0[k] = u.open[k] = u.mask1[k] = 0;
+            if (left ? row < L && j <= row : j < L && d < q.dv) {
+                if (left) {
+                    const long long o = (at + row) * kChunk + j;
+                    u.own0[k] = q.w_x0[o]; u.open[k] = q.w_open[o]; u.mask1[k] = q.a_w[1][o];
+                } else {
+                    const long long o = b * q.v.b + h * q.v.h + (t0 + j) * q.v.t + d, oa = (at + j) * q.dv + d;
+                    u.mask1[k] = q.a_v[1][oa];
+                    u.own0[k] = q.v.p[0][o] + q.recv_v[0][oa];
+                    u.open[k] = q.v.p[1][o] - u.mask1[k] + q.recv_v[1][oa];
+                }
+            }
+        }
+        multiply_unit(s, u, z0, z1);
+        for (int k0 = 0; k0 < q.dk; k0 += 64) {
+            const int k = k0 + kb * kUnit, n = q.dk - k;
+            if (left) {
+                const long long o = b * q.q.b + h * q.q.h + (t0 + row) * q.q.t + k, oa = (at + row) * q.dk + k;
+                const u64 f = row < L ? (u64)(int64_t)pow[row + 1] : 0;
+                open_unit<true>(u, q.q.p[0] + o, q.q.p[1] + o, 1, q.a_qd[0] + oa, q.a_qd[1] + oa, 1, row < L ? n : 0, [&](int) { return f; },
+                                q.bits, n0 == 0 ? box0 : nullptr, box1, kThreads);
+            } else {
+                const int d = n0 + row;
+#pragma unroll
+                for (int i = 0; i < kUnit; ++i) {
+                    u.own0[i] = u.open[i] = u.mask1[i] = 0;
+                    if (d >= q.dv || i >= n) continue;
+                    const long long o = ((bh * q.chunks + chunk) * q.dk + k + i) * q.dv + d;
+                    u.own0[i] = q.u[0][o]; u.open[i] = q.u[1][o]; u.mask1[i] = q.a_s[1][o];
+                }
+            }
+            multiply_unit(s, u, z0, z1);
+        }
+        each_word([&](int r, int i, int j) {
+            if (i >= L || n0 + j >= q.dv) return;
+            const long long oc = (at + i) * q.dv + n0 + j, o = b * q.ob + h * q.oh + (t0 + i) * q.ot + n0 + j;
+            q.o[0][o] = rescaled<0>(q.c_o[0][oc] + z0[r], q.bits);
+            q.o[1][o] = rescaled<1>(q.c_o[1][oc] + z1[r], q.bits);
+        });
+    }
+}
+
+// ---- one token
+struct StepArgs {
+    Rows q, k, v;
+    const u64 *a_q[2], *a_k[2], *a_v[2], *a_s[2], *c_u[2], *c_o[2], *state[2];
+    u64 *o[2]; long long ob, oh;
+    u64* state_out[2];
+    const int32_t* decay;
+    u64* box;
+    int B, H, dk, dv, bits, slices;
+};
+constexpr int kSlice = 16;                    // columns of the state in a workgroup
+constexpr int kStepBoxes = 2048;
+constexpr int kMaxD = MPC_ATTENTION_MAX_D;
+
+constexpr size_t kStepBoxWords = (size_t)kMaxD * kSlice + 2 * kMaxD + kSlice;   // per direction: state, k and q, v
+
+__global__ __launch_bounds__(256) void k_step(StepArgs q)
+{
+    __shared__ u64 part[2][16][kSlice];
+    __shared__ u64 kq[2][3][kMaxD];           // k, q: party 0's operand, opened words, party 1's mask
+    const int col = threadIdx.x % kSlice, group = threadIdx.x / kSlice;
+    u64* const box = q.box + (size_t)blockIdx.x * 2 * kStepBoxWords;
+    const long long jobs = (long long)q.B * q.H * q.slices;
+    for (long long job = blockIdx.x; job < jobs; job += gridDim.x) {
+        const long long bh = job / q.slices;
+        const int slice = (int)(job % q.slices), e = slice * kSlice + col, b = (int)(bh / q.H), h = (int)(bh % q.H);
+        const u64 f = (u64)(int64_t)q.decay[h * (kChunk + 1) + 1];
+        {
+            const int which = threadIdx.x / kMaxD, d = threadIdx.x % kMaxD;
+            const Rows& x = which ? q.q : q.k;
+            const u64* const* a = which ? q.a_q : q.a_k;
+            if (d < q.dk) {
+                const long long o = b * x.b + h * x.h + d, oa = bh * q.dk + d;
+                const u64 x0 = x.p[0][o], m1 = a[1][oa], e1 = x.p[1][o] - m1, e0 = x0 - a[0][oa];
+                if (slice == 0) {
+                    u64* const to = box + kMaxD * kSlice + which * kMaxD + d;
+                    to[0] = e1; to[kStepBoxWords] = e0;
+                }
+                kq[which][0][d] = x0 + e1; kq[which][1][d] = e0 + e1; kq[which][2][d] = m1;
+            }
+        }
+        __syncthreads();
+        u64 z0 = 0, z1 = 0;
+        if (e < q.dv) {
+            const long long ov = b * q.v.b + h * q.v.h + e, oav = bh * q.dv + e;
+            const u64 v0 = q.v.p[0][ov], av1 = q.a_v[1][oav], f0 = v0 - q.a_v[0][oav], f1 = q.v.p[1][ov] - av1;
+            const u64 y0 = v0 + f1, fv = f0 + f1;
+            if (group == 0) {
+                u64* const to = box + kMaxD * kSlice + 2 * kMaxD + col;
+                to[0] = f1; to[kStepBoxWords] = f0;
+            }
+            for (int d = group; d < q.dk; d += 16) {
+                const long long os = (bh * q.dk + d) * q.dv + e;
+                const u64 u0 = q.c_u[0][os] + kq[0][0][d] * y0, u1 = q.c_u[1][os] + kq[0][1][d] * av1 + kq[0][2][d] * fv;
+                const u64 s0 = rescaled<0>(q.state[0][os] * f + u0, q.bits), s1 = rescaled<1>(q.state[1][os] * f + u1, q.bits);
+                q.state_out[0][os] = s0; q.state_out[1][os] = s1;
+                const u64 as1 = q.a_s[1][os], e1 = s1 - as1, e0 = s0 - q.a_s[0][os];
+                box[d * kSlice + col] = e1; box[kStepBoxWords + d * kSlice + col] = e0;
+                z0 += kq[1][0][d] * (s0 + e1);
+                z1 += kq[1][1][d] * as1 + kq[1][2][d] * (e0 + e1);
+            }
+        }
+        part[0][group][col] = z0; part[1][group][col] = z1;
+        __syncthreads();
+        if (group < 2 && e < q.dv) {
+            u64 z = q.c_o[group][bh * q.dv + e];
+            for (int g = 0; g < 16; ++g) z += part[group][g][col];
+            q.o[group][b * q.ob + h * q.oh + e] = rescaled(group, z, q.bits);
+        }
+        __syncthreads();
+    }
+}
+
+bool strides_in(const mpc_strides& s) { return s.batch >= 0 && s.token >= 0 && s.head >= 0; }
+
+// words from the first to the last one of [B][T][H][d] with these strides
+size_t extent(const mpc_strides& s, int B, int T, int H, int d)
+{
+    return (size_t)s.batch * (B - 1) + (size_t)s.token * (T - 1) + (size_t)s.head * (H - 1) + d;
+}
+
+// no two of the output's words share a place: in the order of their strides, every axis steps over the ones within it
+bool strides_out(const mpc_strides& s, int B, int T, int H, int d)
+{
+    if (!strides_in(s)) return false;
+    long long st[3] = { s.batch, s.token, s.head }; int n[3] = { B, T, H };
+    for (int i = 0; i < 2; ++i)
+        for (int j = 0; j < 2 - i; ++j)
+            if (st[j] > st[j + 1]) { std::swap(st[j], st[j + 1]); std::swap(n[j], n[j + 1]); }
+    long long within = d;
+    for (int i = 0; i < 3; ++i) {
+        if (n[i] == 1) continue;
+        if (st[i] < within) return false;
+        within = st[i] * (n[i] - 1) + within;
+    }
+    return true;
+}
+
+Rows rows_of(const mpc_cshare& s, const mpc_strides& st) { return Rows{ { s.p[0], s.p[1] }, st.batch, st.token, st.head }; }
+
+bool both(const mpc_cshare& s) { return s.p[0] && s.p[1]; }
+mpc_cshare seen(const mpc_share& s) { return mpc_cshare{ { s.p[0], s.p[1] } }; }
+
+int shape_ok(mpc_ctx* c, int B, int T, int H, int dk, int dv)
+{
+    if (B <= 0 || T <= 0 || H <= 0 || dk <= 0 || dv <= 0) return MPC_EINVAL;
+    if (dk > MPC_ATTENTION_MAX_D || dv > MPC_ATTENTION_MAX_D || (long long)B * H > INT32_MAX || T > INT32_MAX - kChunk) return MPC_ERANGE;
+    return c && c->frac_bits > 30 ? MPC_ERANGE : MPC_OK;       // a decay of one has to fit 31 bits
+}
+
+struct ChunkPlan { size_t recv, w, u, box, total; long long chunks; };
+ChunkPlan plan(int B, int T, int H, int dk, int dv)
+{
+    ChunkPlan p{};
+    const size_t BH = (size_t)B * H;
+    p.chunks = (T + kChunk - 1) / kChunk;
+    p.recv = BH * T * dv; p.w = BH * T * kChunk; p.u = BH * p.chunks * dk * dv; p.box = kBoxes * 2 * kBoxWords;
+    p.total = 2 * align_up(p.recv * 8) + 2 * align_up(p.w * 8) + 2 * align_up(p.u * 8) + align_up(p.box * 8);
+    return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t mpc_linear_attention_workspace_bytes(int B, int T, int H, int dk, int dv)
+{
+    return shape_ok(nullptr, B, T, H, dk, dv) == MPC_OK ? plan(B, T, H, dk, dv).total : 0;
+}
+
+size_t mpc_linear_attention_step_workspace_bytes(int B, int H, int dk, int dv)
+{
+    return shape_ok(nullptr, B, 1, H, dk, dv) == MPC_OK ? (size_t)kStepBoxes * 2 * kStepBoxWords * 8 : 0;
+}
+
+int mpc_linear_attention(mpc_ctx* c, mpc_cshare q, mpc_cshare k, mpc_cshare v, mpc_strides sq, mpc_strides sk, mpc_strides sv,
+                         const int32_t* decay, const mpc_attention_material* m, mpc_cshare state, mpc_share o, mpc_strides so,
+                         mpc_share state_out, int B, int T, int H, int dk, int dv)
+{
+    if (!c || !decay || !m || !both(q) || !both(k) || !both(v) || !both(seen(o))) return MPC_EINVAL;
+    if (!state.p[0] != !state.p[1] || !state_out.p[0] != !state_out.p[1]) return MPC_EINVAL;
+    const mpc_cshare* const mats[] = { &m->a_q, &m->a_k, &m->a_qd, &m->a_kd, &m->a_v, &m->a_w, &m->a_s, &m->c_p, &m->c_u, &m->c_o };
+    for (const mpc_cshare* x : mats) if (!both(*x)) return MPC_EINVAL;
+    MPC_TRY(shape_ok(c, B, T, H, dk, dv));
+    if (!strides_in(sq) || !strides_in(sk) || !strides_in(sv) || !strides_out(so, B, T, H, dv)) return MPC_EINVAL;
+    const ChunkPlan p = plan(B, T, H, dk, dv);
+    const size_t n_o = extent(so, B, T, H, dv) * 8, n_s = (size_t)B * H * dk * dv * 8;
+    const size_t BHT = (size_t)B * H * T * 8;
+    const size_t sizes[] = { BHT * dk, BHT * dk, BHT * dk, BHT * dk, BHT * dv, BHT * kChunk, p.u * 8, BHT * kChunk, p.u * 8, BHT * dv };
+    const mpc_cshare* const in[] = { &q, &k, &v };
+    const size_t n_in[] = { extent(sq, B, T, H, dk) * 8, extent(sk, B, T, H, dk) * 8, extent(sv, B, T, H, dv) * 8 };
+    for (int pass = 0; pass < 2; ++pass) {
+        const mpc_share& out = pass ? state_out : o;
+        const size_t n = pass ? n_s : n_o;
+        if (!out.p[0]) continue;
+        for (int i = 0; i < 3; ++i) if (!outputs_apart(out, n, *in[i], n_in[i], false)) return MPC_EINVAL;
+        for (int i = 0; i < 10; ++i) if (!outputs_apart(out, n, *mats[i], sizes[i], false)) return MPC_EINVAL;
+        if (state.p[0] && !outputs_apart(out, n, state, n_s, pass == 1)) return MPC_EINVAL;
+    }
+    if (state_out.p[0] && !outputs_apart(o, n_o, seen(state_out), n_s, false)) return MPC_EINVAL;
+
+    ChunkArgs a{};
+    a.q = rows_of(q, sq); a.k = rows_of(k, sk); a.v = rows_of(v, sv);
+    a.decay = decay; a.ob = so.batch; a.ot = so.token; a.oh = so.head;
+    WsAlloc ws(c->ws, c->ws_bytes);
+    for (int i = 0; i < 2; ++i) {
+        a.a_q[i] = m->a_q.p[i]; a.a_k[i] = m->a_k.p[i]; a.a_qd[i] = m->a_qd.p[i]; a.a_kd[i] = m->a_kd.p[i]; a.a_v[i] = m->a_v.p[i];
+        a.a_w[i] = m->a_w.p[i]; a.a_s[i] = m->a_s.p[i]; a.c_p[i] = m->c_p.p[i]; a.c_u[i] = m->c_u.p[i]; a.c_o[i] = m->c_o.p[i];
+        a.state[i] = state.p[i]; a.o[i] = o.p[i]; a.state_out[i] = state_out.p[i];
+        a.recv_v[i] = ws.take<u64>(p.recv); a.u[i] = ws.take<u64>(p.u);
+    }
+    a.w_x0 = ws.take<u64>(p.w); a.w_open = ws.take<u64>(p.w); a.box = ws.take<u64>(p.box);
+    if (!ws.ok) return MPC_ENOMEM;
+    a.B = B; a.H = H; a.T = T; a.dk = dk; a.dv = dv; a.chunks = (int)p.chunks; a.bits = c->frac_bits;
+    a.mt = (dk + 63) / 64; a.nt = (dv + 63) / 64;
+    const auto grid = [](long long jobs, long long most) { return dim3((unsigned)(jobs < most ? jobs : most)); };
+    const long long cells = (long long)B * H * p.chunks;
+    MPC_TRY(lane_first(c));
+    k_chunk_open<<<grid(cells * (1 + a.mt * a.nt), kBoxes), kThreads, 0, c->s[0]>>>(a);
+    k_chunk_states<<<grid(((long long)n_s / 8 + 255) / 256, 4096), 256, 0, c->s[0]>>>(a);
+    k_chunk_out<<<grid(cells * a.nt, kBoxes), kThreads, 0, c->s[0]>>>(a);
+    MPC_HIP(c, hipGetLastError());
+    return lane_fanout(c);
+}
+
+int mpc_linear_attention_step(mpc_ctx* c, mpc_cshare q, mpc_cshare k, mpc_cshare v, mpc_strides sq, mpc_strides sk, mpc_strides sv,
+                              const int32_t* decay, const mpc_attention_step_material* m, mpc_cshare state, mpc_share o, mpc_strides so,
+                              mpc_share state_out, int B, int H, int dk, int dv)
+{
+    if (!c || !decay || !m || !both(q) || !both(k) || !both(v) || !both(state) || !both(seen(o)) || !both(seen(state_out))) return MPC_EINVAL;
+    const mpc_cshare* const mats[] = { &m->a_q, &m->a_k, &m->a_v, &m->a_s, &m->c_u, &m->c_o };
+    for (const mpc_cshare* x : mats) if (!both(*x)) return MPC_EINVAL;
+    MPC_TRY(shape_ok(c, B, 1, H, dk, dv));
+    sq.token = sk.token = sv.token = so.token = 0;
+    if (!strides_in(sq) || !strides_in(sk) || !strides_in(sv) || !strides_out(so, B, 1, H, dv)) return MPC_EINVAL;
+    const size_t BH = (size_t)B * H * 8, n_s = BH * dk * dv, n_o = extent(so, B, 1, H, dv) * 8;
+    const size_t sizes[] = { BH * dk, BH * dk, BH * dv, n_s, n_s, BH * dv };
+    const mpc_cshare* const in[] = { &q, &k, &v };
+    const size_t n_in[] = { extent(sq, B, 1, H, dk) * 8, extent(sk, B, 1, H, dk) * 8, extent(sv, B, 1, H, dv) * 8 };
+    for (int pass = 0; pass < 2; ++pass) {
+        const mpc_share& out = pass ? state_out : o;
+        const size_t n = pass ? n_s : n_o;
+        for (int i = 0; i < 3; ++i) if (!outputs_apart(out, n, *in[i], n_in[i], false)) return MPC_EINVAL;
+        for (int i = 0; i < 6; ++i) if (!outputs_apart(out, n, *mats[i], sizes[i], false)) return MPC_EINVAL;
+        if (!outputs_apart(out, n, state, n_s, pass == 1)) return MPC_EINVAL;
+    }
+    if (!outputs_apart(o, n_o, seen(state_out), n_s, false)) return MPC_EINVAL;
+    if (!c->ws || c->ws_bytes < mpc_linear_attention_step_workspace_bytes(B, H, dk, dv)) return MPC_ENOMEM;
+    StepArgs a{};
+    a.q = rows_of(q, sq); a.k = rows_of(k, sk); a.v = rows_of(v, sv);
+    for (int i = 0; i < 2; ++i) {
+        a.a_q[i] = m->a_q.p[i]; a.a_k[i] = m->a_k.p[i]; a.a_v[i] = m->a_v.p[i]; a.a_s[i] = m->a_s.p[i];
+        a.c_u[i] = m->c_u.p[i]; a.c_o[i] = m->c_o.p[i]; a.state[i] = state.p[i]; a.o[i] = o.p[i]; a.state_out[i] = state_out.p[i];
+    }
+    a.ob = so.batch; a.oh = so.head; a.decay = decay; a.box = reinterpret_cast<u64*>(c->ws);
+    a.B = B; a.H = H; a.dk = dk; a.dv = dv; a.bits = c->frac_bits; a.slices = (dv + kSlice - 1) / kSlice;
+    const long long jobs = (long long)B * H * a.slices;
+    MPC_TRY(lane_first(c));
+    k_step<<<dim3((unsigned)(jobs < kStepBoxes ? jobs : kStepBoxes)), 256, 0, c->s[0]>>>(a);
+    MPC_HIP(c, hipGetLastError());
+    return lane_fanout(c);
+}
+
+}  // extern "C"

@@ -117,6 +117,55 @@ def matmul_backward(lane: "mpc.Lane", g, fwd: dict, g_std: float = 0.5) -> dict:
     return d
 
 
+def _folded_addend(lane: "mpc.Lane", g, products):
+    """Shares of the sum of A B over (a, b) mask sharings, party 0's own a_0 b_0 taken off (mpc_linear_attention's addends)."""
+    whole = lambda s: (s[0] + s[1]).contiguous()
+    lane.wait_torch()
+    C = sum(_ring_product(lane, whole(a), whole(b)) for a, b in products)
+    own = sum(_ring_product(lane, a[0].contiguous(), b[0].contiguous()) for a, b in products)
+    c0, c1 = share(g, C)
+    return c0 - own, c1
+
+
+def _ring_product(lane: "mpc.Lane", A, B):
+    """Batched ring product over all leading axes, waited for."""
+    lane.wait_torch()
+    Z = lane.ring_matmul(A.reshape((-1,) + tuple(A.shape[-2:])), B.reshape((-1,) + tuple(B.shape[-2:])))
+    lane.sync()
+    return Z.view(tuple(A.shape[:-1]) + (B.shape[-1],))
+
+
+def attention_material(lane: "mpc.Lane", g, B, H, T, dk, dv) -> dict:
+    """Masks and addends of mpc_linear_attention (a prompt of T tokens)."""
+    dev, N, C = lane.device, B * H, mpc.ATTENTION_CHUNK
+    nc = -(-T // C)
+    mask = lambda *shape: tuple(rand_words(g, shape, dev) for _ in range(2))
+    m = {n: mask(N, T, dk) for n in ("a_q", "a_k", "a_qd", "a_kd")}
+    m["a_v"], m["a_s"], m["a_w"] = mask(N, T, dv), mask(N, nc, dk, dv), mask(N, T, C)
+    below = (torch.arange(C, device=dev) <= (torch.arange(T, device=dev) % C)[:, None]).to(torch.int64)
+    chunked = lambda s: tuple(torch.nn.functional.pad(t, (0, 0, 0, -T % C)).view(N, nc, C, t.shape[-1]) for t in s)
+    turned = lambda s: tuple(t.transpose(-1, -2) for t in s)
+    tokens = lambda s: tuple(t.reshape(N, nc * C, t.shape[-1])[:, :T].contiguous() for t in s)
+    q, k, qd, kd, v = (chunked(m[n]) for n in ("a_q", "a_k", "a_qd", "a_kd", "a_v"))
+    m["c_p"] = tokens(_folded_addend(lane, g, [(q, turned(k))]))
+    m["c_u"] = _folded_addend(lane, g, [(turned(kd), v)])
+    m["c_o"] = tokens(_folded_addend(lane, g, [(chunked(tuple(t * below for t in m["a_w"])), v), (qd, m["a_s"])]))
+    torch.cuda.synchronize(dev)
+    return m
+
+
+def attention_step_material(lane: "mpc.Lane", g, B, H, dk, dv) -> dict:
+    """Masks and addends of mpc_linear_attention_step (one token of every sequence)."""
+    dev = lane.device
+    mask = lambda *shape: tuple(rand_words(g, shape, dev) for _ in range(2))
+    m = dict(a_q=mask(B, H, dk), a_k=mask(B, H, dk), a_v=mask(B, H, dv), a_s=mask(B, H, dk, dv))
+    at = lambda s, axis: tuple(t.unsqueeze(axis) for t in s)
+    m["c_u"] = _folded_addend(lane, g, [(at(m["a_k"], -1), at(m["a_v"], -2))])
+    m["c_o"] = tuple(t.squeeze(-2) for t in _folded_addend(lane, g, [(at(m["a_q"], -2), m["a_s"])]))
+    torch.cuda.synchronize(dev)
+    return m
+
+
 def mul_triple(g, n: int, device):
     """Element-wise multiplication triple on n words."""
     a = rand_words(g, (n,), device); b = rand_words(g, (n,), device)

@@ -48,6 +48,24 @@ class Relu3Material(ctypes.Structure):
                 ("rb", _P8 * 3), ("ra", CShare3), ("ma", CShare3), ("mb", CShare3), ("mc", CShare3)]
 
 
+class Strides(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+_ATTENTION_MASKS = ("a_q", "a_k", "a_qd", "a_kd", "a_v", "a_w", "a_s", "c_p", "c_u", "c_o")
+_STEP_MASKS = ("a_q", "a_k", "a_v", "a_s", "c_u", "c_o")
+
+
+class AttentionMaterial(ctypes.Structure):
+    _fields_ = [(n, CShare) for n in _ATTENTION_MASKS]
+
+
+class AttentionStepMaterial(ctypes.Structure):
+    _fields_ = [(n, CShare) for n in _STEP_MASKS]
+
+
+ATTENTION_CHUNK, ATTENTION_MAX_D, MAX_BUCKETS = 64, 128, 4096
+
 N_AND_TRIPLES3 = 13
 
 EXPORTS = [
@@ -77,6 +95,8 @@ EXPORTS = [
     "mpc_conv2d3_grad_x_workspace_bytes", "mpc_conv2d3_grad_w_workspace_bytes", "mpc_conv2d3_grad_x", "mpc_conv2d3_grad_w",
     "mpc_add3", "mpc_sub3", "mpc_mul3_workspace_bytes", "mpc_mul3", "mpc_relu3_backward", "mpc_maxpool3_signs",
     "mpc_maxpool3_backward_workspace_bytes", "mpc_maxpool3_backward",
+    "mpc_position_bias", "mpc_position_bias_grad", "mpc_matvec4", "mpc_linear_attention_workspace_bytes", "mpc_linear_attention",
+    "mpc_linear_attention_step_workspace_bytes", "mpc_linear_attention_step",
 ]
 
 _lib = None
@@ -197,6 +217,13 @@ def lib():
                                      POINTER(_P64 * 3), POINTER(_P64 * 3)] + [c_int] * 5
     L.mpc_maxpool3_backward_workspace_bytes.argtypes = [c_int] * 4; L.mpc_maxpool3_backward_workspace_bytes.restype = c_size_t
     L.mpc_maxpool3_backward.argtypes = [c_void_p] + [CShare3] * 10 + [c_int] * 4
+    L.mpc_position_bias.argtypes = [c_void_p, CShare, CShare, c_void_p, CShare] + [c_int] * 5
+    L.mpc_position_bias_grad.argtypes = [c_void_p, CShare, c_void_p, CShare, CShare] + [c_int] * 5
+    L.mpc_matvec4.argtypes = [c_void_p, CShare, c_void_p, c_void_p, CShare] + [c_int] * 5
+    L.mpc_linear_attention_workspace_bytes.argtypes = [c_int] * 5; L.mpc_linear_attention_workspace_bytes.restype = c_size_t
+    L.mpc_linear_attention.argtypes = [c_void_p] + [CShare] * 3 + [Strides] * 3 + [c_void_p, POINTER(AttentionMaterial), CShare, CShare, Strides, CShare] + [c_int] * 5
+    L.mpc_linear_attention_step_workspace_bytes.argtypes = [c_int] * 4; L.mpc_linear_attention_step_workspace_bytes.restype = c_size_t
+    L.mpc_linear_attention_step.argtypes = [c_void_p] + [CShare] * 3 + [Strides] * 3 + [c_void_p, POINTER(AttentionStepMaterial), CShare, CShare, Strides, CShare] + [c_int] * 4
     _lib = L
     return L
 
@@ -286,6 +313,48 @@ def _material3(mat: dict, n: int, packed: bool = False) -> Relu3Material:
                                  (f" ({'packed' if packed else '[13][n]'} layout)" if key.startswith("and") else ""))
             addresses.append(_address(t, dtype, noted))
     return Relu3Material.from_buffer_copy(_pack_material3(*addresses))
+
+
+def _dense(t, shape, dtype, device, name):
+    """Checked device address of a dense tensor."""
+    if t.shape != shape or t.dtype is not dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"'{name}': contiguous {dtype} tensor of shape {list(shape)} on {device} expected, "
+                         f"got {t.dtype} {list(t.shape)} on {t.device}")
+    _noted().append(t)
+    return t.data_ptr()
+
+
+def _dense_share(pair, shape, device, name):
+    if len(pair) != 2:
+        raise ValueError(f"'{name}': a sharing is a pair of tensors")
+    return CShare.from_buffer_copy(_pack2(_dense(pair[0], shape, torch.int64, device, name), _dense(pair[1], shape, torch.int64, device, name)))
+
+
+def _heads_share(pair, shape, device, name):
+    """Addresses and strides of a sharing of [B, (T,) H, d]; the last axis is dense, the others lie as they lie."""
+    if len(pair) != 2:
+        raise ValueError(f"'{name}': a sharing is a pair of tensors")
+    a, b = pair
+    st = a.stride()
+    for t in pair:
+        if t.shape != shape or t.dtype is not torch.int64 or t.device != device or t.stride() != st or (st[-1] != 1 and shape[-1] != 1):
+            raise ValueError(f"'{name}': int64 tensors of shape {list(shape)} on {device}, dense in the last axis and with the same "
+                             f"strides for both shares expected, got {t.dtype} {list(t.shape)} strides {t.stride()} on {t.device}")
+    _noted().extend(pair)
+    strides = Strides(st[0], st[1], st[2]) if len(shape) == 4 else Strides(st[0], 0, st[1])
+    return CShare.from_buffer_copy(_pack2(a.data_ptr(), b.data_ptr())), strides
+
+
+def _attention_material(struct_type, names, mat, shapes, device):
+    missing = [n for n in names if n not in mat]
+    if missing:
+        raise ValueError(f"material lacks {missing}")
+    words = []
+    for n in names:
+        if len(mat[n]) != 2:
+            raise ValueError(f"material '{n}': a sharing is a pair of tensors")
+        words += [_dense(t, shapes[n], torch.int64, device, n) for t in mat[n]]
+    return struct_type.from_buffer_copy(struct.pack(f"{len(words)}Q", *words))
 
 
 def to_device(arr, device="cuda:0"):
@@ -914,6 +983,91 @@ class Lane:
         return y
 
     # -- dealer helpers (offline phase stand-in)
+    # -- attention without a softmax, public 4-bit weights
+    def position_bias(self, scores, table, buckets, out=None):
+        """scores [B, H, Tq, Tk] + table [n, H] at the public bucket of every pair: buckets int32 [Tq + Tk - 1], entry
+        j - i + Tq - 1 of query i and key j; an entry outside [0, n) masks its pairs (zero).  out may be scores."""
+        B, H, Tq, Tk = scores[0].shape
+        n = table[0].shape[0]
+        out = out if out is not None else (torch.empty_like(scores[0]), torch.empty_like(scores[1]))
+        shape = scores[0].shape
+        s, t, o = (_dense_share(scores, shape, self.device, "scores"), _dense_share(table, (n, H), self.device, "table"),
+                   _dense_share(out, shape, self.device, "out"))
+        m = _dense(buckets, (Tq + Tk - 1,), torch.int32, self.device, "buckets")
+        self._check(lib().mpc_position_bias(self._h, s, t, m, o, B, H, Tq, Tk, n))
+        return out
+
+    def position_bias_grad(self, g, buckets, n_buckets, out=None, scores_out=None):
+        """Gradient of position_bias for its output's g: (table's [n_buckets, H], scores').  The scores' gradient is g with
+        zeros at masked pairs; it is written to scores_out (may be g), or not at all if that is None."""
+        B, H, Tq, Tk = g[0].shape
+        if out is None:
+            out = tuple(torch.empty((n_buckets, H), dtype=torch.int64, device=self.device) for _ in range(2))
+        shape = g[0].shape
+        s, o = _dense_share(g, shape, self.device, "g"), _dense_share(out, (n_buckets, H), self.device, "out")
+        so = _dense_share(scores_out, shape, self.device, "scores_out") if scores_out is not None else CShare()
+        m = _dense(buckets, (Tq + Tk - 1,), torch.int32, self.device, "buckets")
+        self._check(lib().mpc_position_bias_grad(self._h, s, m, o, so, B, H, Tq, Tk, n_buckets))
+        return out, scores_out
+
+    def matvec4(self, x, w, scales, group, scale_bits=16, out=None):
+        """x [M, K] times public 4-bit weights: w uint8 [N, 16 ceil(K / 32)] (attention.pack_weights4), scales int32
+        [N, ceil(K / group)] with scale_bits fraction bits.  z [M, N] in x's fixed point."""
+        M, K = x[0].shape
+        N = w.shape[0]
+        out = out if out is not None else tuple(torch.empty((M, N), dtype=torch.int64, device=self.device) for _ in range(2))
+        if group <= 0:
+            raise ValueError(f"group: a positive number of columns expected, got {group}")
+        xs, zs = _dense_share(x, (M, K), self.device, "x"), _dense_share(out, (M, N), self.device, "out")
+        wp = _dense(w, (N, -(-K // 32) * 16), torch.uint8, self.device, "w")
+        sp = _dense(scales, (N, -(-K // group)), torch.int32, self.device, "scales")
+        self._check(lib().mpc_matvec4(self._h, xs, wp, sp, zs, M, K, N, group, scale_bits))
+        return out
+
+    def linear_attention(self, q, k, v, decay, mat, state=None, out=None, state_out=None):
+        """Linear attention over T tokens in chunks of 64: q, k [B, T, H, dk], v [B, T, H, dv], any strides but a dense last
+        axis; decay int32 [H, 65] (attention.decay_powers); mat as dealer.attention_material deals it; state
+        [B, H, dk, dv] before the first token (None: zero).  Returns (o [B, T, H, dv], state after the last token);
+        state_out may be state."""
+        B, T, H, dk = q[0].shape
+        dv = v[0].shape[-1]
+        dev, BH, nc = self.device, B * H, -(-T // ATTENTION_CHUNK)
+        empty = lambda *shape: tuple(torch.empty(shape, dtype=torch.int64, device=dev) for _ in range(2))
+        out = out if out is not None else empty(B, T, H, dv)
+        state_out = state_out if state_out is not None else empty(B, H, dk, dv)
+        self.reserve(lib().mpc_linear_attention_workspace_bytes(B, T, H, dk, dv))
+        (qs, sq), (ks, sk) = _heads_share(q, (B, T, H, dk), dev, "q"), _heads_share(k, (B, T, H, dk), dev, "k")
+        (vs, sv), (os_, so) = _heads_share(v, (B, T, H, dv), dev, "v"), _heads_share(out, (B, T, H, dv), dev, "out")
+        rows, cells = (BH, T, dk), (BH, nc, dk, dv)
+        shapes = dict(a_q=rows, a_k=rows, a_qd=rows, a_kd=rows, a_v=(BH, T, dv), a_w=(BH, T, ATTENTION_CHUNK), a_s=cells,
+                      c_p=(BH, T, ATTENTION_CHUNK), c_u=cells, c_o=(BH, T, dv))
+        m = _attention_material(AttentionMaterial, _ATTENTION_MASKS, mat, shapes, dev)
+        st = _dense_share(state, (B, H, dk, dv), dev, "state") if state is not None else CShare()
+        sn = _dense_share(state_out, (B, H, dk, dv), dev, "state_out")
+        d = _dense(decay, (H, ATTENTION_CHUNK + 1), torch.int32, dev, "decay")
+        self._check(lib().mpc_linear_attention(self._h, qs, ks, vs, sq, sk, sv, d, byref(m), st, os_, so, sn, B, T, H, dk, dv))
+        return out, state_out
+
+    def linear_attention_step(self, q, k, v, decay, mat, state, out=None, state_out=None):
+        """One token of linear_attention: q, k [B, H, dk], v [B, H, dv], state [B, H, dk, dv]; mat as
+        dealer.attention_step_material deals it.  Returns (o [B, H, dv], new state); state_out may be state."""
+        B, H, dk = q[0].shape
+        dv = v[0].shape[-1]
+        dev = self.device
+        empty = lambda *shape: tuple(torch.empty(shape, dtype=torch.int64, device=dev) for _ in range(2))
+        out = out if out is not None else empty(B, H, dv)
+        state_out = state_out if state_out is not None else empty(B, H, dk, dv)
+        self.reserve(lib().mpc_linear_attention_step_workspace_bytes(B, H, dk, dv))
+        (qs, sq), (ks, sk) = _heads_share(q, (B, H, dk), dev, "q"), _heads_share(k, (B, H, dk), dev, "k")
+        (vs, sv), (os_, so) = _heads_share(v, (B, H, dv), dev, "v"), _heads_share(out, (B, H, dv), dev, "out")
+        cell = (B, H, dk, dv)
+        shapes = dict(a_q=(B, H, dk), a_k=(B, H, dk), a_v=(B, H, dv), a_s=cell, c_u=cell, c_o=(B, H, dv))
+        m = _attention_material(AttentionStepMaterial, _STEP_MASKS, mat, shapes, dev)
+        st, sn = _dense_share(state, cell, dev, "state"), _dense_share(state_out, cell, dev, "state_out")
+        d = _dense(decay, (H, ATTENTION_CHUNK + 1), torch.int32, dev, "decay")
+        self._check(lib().mpc_linear_attention_step(self._h, qs, ks, vs, sq, sk, sv, d, byref(m), st, os_, so, sn, B, H, dk, dv))
+        return out, state_out
+
     def ring_matmul(self, L, R):
         shp = L.shape
         batch = 1 if len(shp) == 2 else shp[0]
