@@ -569,9 +569,11 @@ int mpc_matvec4(mpc_ctx* ctx, mpc_cshare x, const uint8_t* w, const int32_t* sca
  *     a_s [BH][chunks][dk][dv] (mask of the state before each chunk);
  *     c_p [BH][T][64] of a_q a_k^T, c_u [BH][chunks][dk][dv] of a_kd^T a_v, c_o [BH][T][dv] of a_w a_v + a_qd a_s
  *   step: a_q, a_k [BH][dk], a_v [BH][dv], a_s [BH][dk][dv] (mask of S'); c_u [BH][dk][dv] of a_k a_v^T, c_o [BH][dv] of a_q a_s
- * MPC_ERANGE: dk or dv beyond MPC_ATTENTION_MAX_D, frac_bits > 30, B * H beyond 2^31.  Workspace: the queries. */
+ * MPC_ERANGE: dk or dv beyond MPC_ATTENTION_MAX_D, frac_bits > 30, B * H beyond 2^31, an input token stride of a prompt beyond
+ * MPC_ATTENTION_MAX_TOKEN_STRIDE.  Workspace: the queries. */
 #define MPC_ATTENTION_CHUNK 64
 #define MPC_ATTENTION_MAX_D 128
+#define MPC_ATTENTION_MAX_TOKEN_STRIDE 4194303     /* of q, k, v of a prompt, in words */
 typedef struct { int64_t batch, token, head; } mpc_strides;
 typedef struct { mpc_cshare a_q, a_k, a_qd, a_kd, a_v, a_w, a_s, c_p, c_u, c_o; } mpc_attention_material;
 typedef struct { mpc_cshare a_q, a_k, a_v, a_s, c_u, c_o; } mpc_attention_step_material;

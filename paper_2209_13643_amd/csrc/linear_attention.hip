@@ -14,6 +14,7 @@
 // party 0 has c_0 + (x_0 + e_1)(y_0 + f_1), party 1 has c_1 + e b_1 + a_1 f.  The exchange is by remote store: a masked word is
 // stored into the peer's receive buffer and used as it passes.
 #include "attention.h"
+#include "digits.h"
 
 namespace {
 
@@ -21,6 +22,7 @@ constexpr int kChunk = MPC_ATTENTION_CHUNK;   // 64
 constexpr int kThreads = 512;
 constexpr int kUnit = 16;                     // words along the contraction that a thread brings
 constexpr int kBoxes = 512;                   // workgroups of a launch, each with receive buffers of its own
+constexpr long long kMaxStride = MPC_ATTENTION_MAX_TOKEN_STRIDE;   // 64 tokens stay below 2^31 bytes
 constexpr size_t kBoxWords = (size_t)kThreads * kUnit;   // per direction
 
 struct Rows { const u64* p[2]; long long b, t, h; };     // words of (batch, token, head) at p + b*b + t*t + h*h
@@ -39,80 +41,186 @@ struct ChunkArgs {
     int mt, nt;                               // tiles of 64 along dk and dv
 };
 
-// The words of a thread's unit: 16 along the contraction of one row.
-struct Unit { u64 own0[kUnit], open[kUnit], mask1[kUnit]; };   // party 0's operand x_0 + e_1; e; a_1
+// A thread brings 16 words of an operand tile of 64 rows by 64 along the contraction, as four quads along the contraction: of
+// four rows where a row's words are adjacent in memory (four lanes read 128 bytes), else of one row, neighbouring lanes on
+// neighbouring rows.  The first four waves bring the left operand, the others the right one.
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64)); }
+template <bool ADJACENT> struct Place {
+    __device__ __forceinline__ static int row(int i) { const int l = threadIdx.x % 64; return ADJACENT ? i * 16 + l / 4 : l; }
+    __device__ __forceinline__ static int k(int i) { return wave_id() % 4 * 16 + (ADJACENT ? (int)threadIdx.x % 4 : i) * 4; }
+};
+typedef u64 Words[4][4];
 
-// A masked operand: x, a of both parties at offset k*kx / k*ka from a row's first word; n of the 16 words are there.
-// power(k): public factor and rescale before masking, or none.
-template <bool DECAY, class Power>
-__device__ __forceinline__ void open_unit(Unit& u, const u64* x0, const u64* x1, long long kx, const u64* a0, const u64* a1, long long ka,
-                                          int n, Power power, int bits, u64* to0, u64* to1, long long kt)
+__device__ __forceinline__ u64 word_at(const u64* base, unsigned bytes) { return *reinterpret_cast<const u64*>(reinterpret_cast<const u8*>(base) + bytes); }
+
+// Word (row, k) lies at base + row*rs + k*ks, one of the two strides being 1.  Rows and columns that are not there repeat the
+// last one (its value is not used).  Offsets from the tile's first word are below 2^31 bytes (kMaxStride).
+template <bool ADJACENT>
+__device__ __forceinline__ void fetch(Words& w, const u64* base, long long stride, int rows, int cols, int from = 0, int to = 4)
 {
 #pragma unroll
-    for (int k = 0; k < kUnit; ++k) {
-        u.own0[k] = u.open[k] = u.mask1[k] = 0;
-        if (k >= n) continue;
-        u64 w0 = x0[k * kx], w1 = x1[k * kx];
-        if (DECAY) { const u64 f = power(k); w0 = rescaled<0>(w0 * f, bits); w1 = rescaled<1>(w1 * f, bits); }
-        const u64 m1 = a1[k * ka], e0 = w0 - a0[k * ka], e1 = w1 - m1;
-        if (to0) { to0[k * kt] = e1; to1[k * kt] = e0; }      // the exchange
-        u.own0[k] = w0 + e1; u.open[k] = e1 + e0; u.mask1[k] = m1;
+    for (int i = from; i < to; ++i) {
+        const int row = Place<ADJACENT>::row(i), k = Place<ADJACENT>::k(i);
+        const unsigned r = row < rows ? row : rows - 1;
+        if (ADJACENT) {
+            const unsigned off = r * ((unsigned)stride * 8);
+            if (cols % 4 == 0) {
+                const u8* const at = reinterpret_cast<const u8*>(base) + (off + (unsigned)(k < cols ? k : cols - 4) * 8);
+                const u64x2u lo = *reinterpret_cast<const u64x2u*>(at), hi = *reinterpret_cast<const u64x2u*>(at + 16);
+                w[i][0] = lo.x; w[i][1] = lo.y; w[i][2] = hi.x; w[i][3] = hi.y;
+            } else
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[i][j] = word_at(base, off + (unsigned)(k + j < cols ? k + j : cols - 1) * 8);
+        } else
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[i][j] = word_at(base + (k + j < cols ? k + j : cols - 1) * stride, r * 8);
+    }
+}
+template <bool ADJACENT> __device__ __forceinline__ bool there(int i, int j, int rows, int cols)
+{
+    return Place<ADJACENT>::row(i) < rows && Place<ADJACENT>::k(i) + j < cols;
+}
+
+struct Unit { Words own0, open, mask1; };     // party 0's operand x_0 + e_1; e; a_1
+
+// A masked operand; a word's power(i, j) is a public factor, followed by the rescale (DECAY); sent(i, j, to party 0, to party 1).
+template <bool ADJACENT, bool DECAY, class Power, class Sent>
+__device__ __forceinline__ void open_unit(Unit& u, const u64* x0, const u64* x1, long long stride, const u64* a0, const u64* a1,
+                                          long long a_stride, int rows, int cols, Power power, int bits, Sent sent)
+{
+    Words a;                                  // party 0's mask
+#pragma unroll
+    for (int half = 0; half < 4; half += 2) { // two quads in flight: registers
+        fetch<ADJACENT>(u.own0, x0, stride, rows, cols, half, half + 2);
+        fetch<ADJACENT>(u.open, x1, stride, rows, cols, half, half + 2);
+        fetch<ADJACENT>(a, a0, a_stride, rows, cols, half, half + 2);
+        fetch<ADJACENT>(u.mask1, a1, a_stride, rows, cols, half, half + 2);
+#pragma unroll
+        for (int i = half; i < half + 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                u64 w0 = u.own0[i][j], w1 = u.open[i][j];
+                if (DECAY) { const u64 f = power(i, j); w0 = rescaled<0>(w0 * f, bits); w1 = rescaled<1>(w1 * f, bits); }
+                const bool in = there<ADJACENT>(i, j, rows, cols);
+                const u64 e0 = w0 - a[i][j], e1 = w1 - u.mask1[i][j];
+                if (in) sent(i, j, e1, e0);
+                u.own0[i][j] = in ? w0 + e1 : 0; u.open[i][j] = in ? e0 + e1 : 0; if (!in) u.mask1[i][j] = 0;
+            }
+        __builtin_amdgcn_sched_barrier(0);
     }
 }
 
-// ---- products of 64 x 64 x 64 words: tile words in LDS, left [k][row], right [k][col]
-struct Tile { u64 left[64][64], right[64][64]; };
+// ---- products of 64 x 64 x 64 words on the matrix cores: eight digit planes of an operand tile in LDS, [digit][k/16][row][16]
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+constexpr int kPlane = 64 * 64, kOperand = 8 * kPlane;      // bytes
 
-__device__ __forceinline__ void stage(Tile& s, const u64 (&w)[kUnit])
+template <bool ADJACENT> __device__ __forceinline__ void stage(u8* to, const Words& w)
 {
-    const int t = threadIdx.x % 256, row = t % 64, kb = t / 64;
-    u64 (*const to)[64] = threadIdx.x < 256 ? s.left : s.right;
+    const int kb = threadIdx.x / 64 % 4;
+    if (ADJACENT) {
 #pragma unroll
-    for (int k = 0; k < kUnit; ++k) to[kb * kUnit + k][row] = w[k];
-}
-__device__ __forceinline__ void multiply(const Tile& s, u64 (&z)[8])
-{
-    const int col = threadIdx.x % 64, r0 = threadIdx.x / 64 * 8;
-    for (int k = 0; k < 64; ++k) {
-        const u64 y = s.right[k][col];
+        for (int i = 0; i < 4; ++i) {
+            uint32_t d[8];
+            digits_of_4(w[i], d);
+            u8* const at = to + (kb * 64 + Place<true>::row(i)) * 16 + threadIdx.x % 4 * 4;
 #pragma unroll
-        for (int r = 0; r < 8; ++r) z[r] += s.left[k][r0 + r] * y;
+            for (int q = 0; q < 8; ++q) *reinterpret_cast<uint32_t*>(at + q * kPlane) = d[q];
+        }
+    } else {
+        uint32_t d[4][8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) digits_of_4(w[i], d[i]);
+        u8* const at = to + (kb * 64 + threadIdx.x % 64) * 16;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) *reinterpret_cast<uint4*>(at + q * kPlane) = uint4{ d[0][q], d[1][q], d[2][q], d[3][q] };
     }
 }
-// z0 += own0 own0', z1 += open mask1' + mask1 open'
-__device__ __forceinline__ void multiply_unit(Tile& s, const Unit& u, u64 (&z0)[8], u64 (&z1)[8])
+
+// A wave has 16 rows and two tiles of 16 columns; acc[tile][s] sums the products of digits i + j = s.  One K step of 64 adds at
+// most (s + 1) 2^20 to it.
+struct Sums { i32x4 s[2][8]; };
+__device__ __forceinline__ void clear(Sums& z)
 {
-    const bool left = threadIdx.x < 256;
-    __syncthreads();
-    stage(s, u.own0);
-    __syncthreads();
-    multiply(s, z0);
-    __syncthreads();
-    if (left) stage(s, u.open); else stage(s, u.mask1);
-    __syncthreads();
-    multiply(s, z1);
-    __syncthreads();
-    if (left) stage(s, u.mask1); else stage(s, u.open);
-    __syncthreads();
-    multiply(s, z1);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int s = 0; s < 8; ++s) z.s[t][s] = i32x4{ 0, 0, 0, 0 };
 }
+__device__ __forceinline__ void multiply(const u8* lds, Sums& z)
+{
+    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+    const u8* const l = lds + (lane / 16 * 64 + wave % 4 * 16 + lane % 16) * 16;
+    const u8* const r = lds + kOperand + (lane / 16 * 64 + wave / 4 * 32 + lane % 16) * 16;
+    i32x4 a[8];
+#pragma unroll
+    for (int d = 0; d < 8; ++d) a[d] = *reinterpret_cast<const i32x4*>(l + d * kPlane);
+    i32x4 b0 = *reinterpret_cast<const i32x4*>(r), b1 = *reinterpret_cast<const i32x4*>(r + 256);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        // the next digit's operands are on their way under this one's products, and no further ones: registers
+        const i32x4 c0 = b0, c1 = b1;
+        if (j < 7) { b0 = *reinterpret_cast<const i32x4*>(r + (j + 1) * kPlane); b1 = *reinterpret_cast<const i32x4*>(r + (j + 1) * kPlane + 256); }
+#pragma unroll
+        for (int i = 0; i < 8 - j; ++i) {
+            z.s[0][i + j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[i], c0, z.s[0][i + j], 0, 0, 0);
+            z.s[1][i + j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[i], c1, z.s[1][i + j], 0, 0, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+// z += sum of the digit sums, of one or two K steps: below 2^31 up to acc[1] 2^8
+__device__ __forceinline__ void join(const Sums& a, u64 (&z)[8])
+{
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int low = a.s[t][0][r] + a.s[t][1][r] * 256;
+            const uint32_t high = (uint32_t)a.s[t][4][r] + ((uint32_t)a.s[t][5][r] << 8) + ((uint32_t)a.s[t][6][r] << 16) + ((uint32_t)a.s[t][7][r] << 24);
+            const int64_t w = (int64_t)low + (int64_t)a.s[t][2][r] * 65536 + (int64_t)a.s[t][3][r] * 16777216;
+            z[t * 4 + r] += (u64)w + ((u64)high << 32);
+        }
+}
+
+// z0 += own0 own0', z1 += open mask1' + mask1 open'.  The first two products' operands are in LDS together; the third's take
+// the first one's place.
+template <bool LEFT_ADJACENT, bool RIGHT_ADJACENT>
+__device__ __forceinline__ void multiply_unit(u8* lds, const Unit& u, u64 (&z0)[8], u64 (&z1)[8])
+{
+    __syncthreads();
+    if (wave_id() < 4) { stage<LEFT_ADJACENT>(lds, u.own0); stage<LEFT_ADJACENT>(lds + 2 * kOperand, u.open); }
+    else { stage<RIGHT_ADJACENT>(lds + kOperand, u.own0); stage<RIGHT_ADJACENT>(lds + 3 * kOperand, u.mask1); }
+    __syncthreads();
+    Sums a;
+    clear(a);
+    multiply(lds, a);
+    join(a, z0);
+    __syncthreads();
+    if (wave_id() < 4) stage<LEFT_ADJACENT>(lds, u.mask1); else stage<RIGHT_ADJACENT>(lds + kOperand, u.open);
+    clear(a);
+    multiply(lds + 2 * kOperand, a);
+    __syncthreads();
+    multiply(lds, a);
+    join(a, z1);
+}
+// each(index, row, column) of a thread's words of the product
 template <class Each> __device__ __forceinline__ void each_word(Each each)
 {
-    const int col = threadIdx.x % 64, r0 = threadIdx.x / 64 * 8;
+    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
 #pragma unroll
-    for (int r = 0; r < 8; ++r) each(r, r0 + r, col);
+    for (int r = 0; r < 8; ++r) each(r, wave % 4 * 16 + lane / 16 * 4 + r % 4, wave / 4 * 32 + r / 4 * 16 + lane % 16);
 }
 
-struct NoPower { __device__ u64 operator()(int) const { return 1; } };
+struct NoPower { __device__ u64 operator()(int, int) const { return 1; } };
 
 // P and W of a chunk, or one tile of its U.
 __global__ __launch_bounds__(kThreads) void k_chunk_open(ChunkArgs q)
 {
-    __shared__ Tile s;
-    const int t = threadIdx.x % 256, row = t % 64, kb = t / 64;
-    const bool left = threadIdx.x < 256;
+    extern __shared__ __attribute__((aligned(16))) u8 lds[];          // 4 kOperand
+    const bool left = wave_id() < 4;
     u64* const box0 = q.box + blockIdx.x * 2 * kBoxWords + threadIdx.x;
     u64* const box1 = box0 + kBoxWords;
+    const auto to_box = [&](int i, int j, u64 to0, u64 to1) { box0[(i * 4 + j) * kThreads] = to0; box1[(i * 4 + j) * kThreads] = to1; };
     const long long jobs = (long long)q.B * q.H * q.chunks * (1 + q.mt * q.nt);
     for (long long job = blockIdx.x; job < jobs; job += gridDim.x) {
         const int kind = (int)(job % (1 + q.mt * q.nt));
@@ -126,11 +234,10 @@ __global__ __launch_bounds__(kThreads) void k_chunk_open(ChunkArgs q)
             const Rows& x = left ? q.q : q.k;
             const u64* const* a = left ? q.a_q : q.a_k;
             for (int k0 = 0; k0 < q.dk; k0 += 64) {
-                const int k = k0 + kb * kUnit, n = row < L ? q.dk - k : 0;
-                const long long o = b * x.b + h * x.h + (t0 + row) * x.t + k, oa = (at + row) * q.dk + k;
+                const long long o = b * x.b + h * x.h + t0 * x.t + k0, oa = at * q.dk + k0;
                 Unit u;
-                open_unit<false>(u, x.p[0] + o, x.p[1] + o, 1, a[0] + oa, a[1] + oa, 1, n, NoPower{}, 0, box0, box1, kThreads);
-                multiply_unit(s, u, z0, z1);
+                open_unit<true, false>(u, x.p[0] + o, x.p[1] + o, x.t, a[0] + oa, a[1] + oa, q.dk, L, q.dk - k0, NoPower{}, 0, to_box);
+                multiply_unit<true, true>(lds, u, z0, z1);
             }
             each_word([&](int r, int i, int j) {
                 if (i >= L || j > i) return;
@@ -139,25 +246,27 @@ __global__ __launch_bounds__(kThreads) void k_chunk_open(ChunkArgs q)
                 const u64 w0 = rescaled<0>(rescaled<0>(q.c_p[0][o] + z0[r], q.bits) * f, q.bits);
                 const u64 w1 = rescaled<1>(rescaled<1>(q.c_p[1][o] + z1[r], q.bits) * f, q.bits);
                 const u64 e0 = w0 - q.a_w[0][o], e1 = w1 - q.a_w[1][o];
-                box0[(long long)r * kThreads] = e1; box1[(long long)r * kThreads] = e0;
+                box0[r * kThreads] = e1; box1[r * kThreads] = e0;
                 q.w_x0[o] = w0 + e1; q.w_open[o] = e0 + e1;
             });
         } else {
-            const int m0 = (kind - 1) / q.nt * 64, n0 = (kind - 1) % q.nt * 64;
-            const int j = kb * kUnit, n = L - j;                  // contraction over the chunk's tokens
+            const int m0 = (kind - 1) / q.nt * 64, n0 = (kind - 1) % q.nt * 64;      // contraction over the chunk's tokens
             Unit u;
             if (left) {
-                const int d = m0 + row;
-                const long long o = b * q.k.b + h * q.k.h + (t0 + j) * q.k.t + d, oa = (at + j) * q.dk + d;
-                open_unit<true>(u, q.k.p[0] + o, q.k.p[1] + o, q.k.t, q.a_kd[0] + oa, q.a_kd[1] + oa, q.dk, d < q.dk ? n : 0,
-                                [&](int k) { return (u64)(int64_t)pow[L - 1 - j - k]; }, q.bits, n0 == 0 ? box0 : nullptr, box1, kThreads);
+                const long long o = b * q.k.b + h * q.k.h + t0 * q.k.t + m0, oa = at * q.dk + m0;
+                open_unit<false, true>(u, q.k.p[0] + o, q.k.p[1] + o, q.k.t, q.a_kd[0] + oa, q.a_kd[1] + oa, q.dk, q.dk - m0, L,
+                    [&](int i, int j) { const int k = Place<false>::k(i) + j; return (u64)(int64_t)pow[k < L ? L - 1 - k : 0]; }, q.bits,
+                    [&](int i, int j, u64 to0, u64 to1) { if (n0 == 0) to_box(i, j, to0, to1); });
             } else {
-                const int d = n0 + row;
-                const long long o = b * q.v.b + h * q.v.h + (t0 + j) * q.v.t + d, oa = (at + j) * q.dv + d;
-                open_unit<false>(u, q.v.p[0] + o, q.v.p[1] + o, q.v.t, q.a_v[0] + oa, q.a_v[1] + oa, q.dv, d < q.dv ? n : 0, NoPower{}, 0,
-                                 m0 == 0 ? q.recv_v[0] + oa : nullptr, q.recv_v[1] + oa, q.dv);
+                const long long o = b * q.v.b + h * q.v.h + t0 * q.v.t + n0, oa = at * q.dv + n0;
+                open_unit<false, false>(u, q.v.p[0] + o, q.v.p[1] + o, q.v.t, q.a_v[0] + oa, q.a_v[1] + oa, q.dv, q.dv - n0, L, NoPower{}, 0,
+                    [&](int i, int j, u64 to0, u64 to1) {
+                        if (m0) return;
+                        const long long to = oa + Place<false>::row(i) + (long long)(Place<false>::k(i) + j) * q.dv;
+                        q.recv_v[0][to] = to0; q.recv_v[1][to] = to1;
+                    });
             }
-            multiply_unit(s, u, z0, z1);
+            multiply_unit<false, false>(lds, u, z0, z1);
             each_word([&](int r, int i, int jj) {
                 const int d = m0 + i, e = n0 + jj;
                 if (d >= q.dk || e >= q.dv) return;
@@ -193,9 +302,8 @@ __global__ __launch_bounds__(256) void k_chunk_states(ChunkArgs q)
 // O of a chunk, 64 columns of dv: first the part within the chunk, then the state's.
 __global__ __launch_bounds__(kThreads) void k_chunk_out(ChunkArgs q)
 {
-    __shared__ Tile s;
-    const int t = threadIdx.x % 256, row = t % 64, kb = t / 64;
-    const bool left = threadIdx.x < 256;
+    extern __shared__ __attribute__((aligned(16))) u8 lds[];          // 4 kOperand
+    const bool left = wave_id() < 4;
     u64* const box0 = q.box + blockIdx.x * 2 * kBoxWords + threadIdx.x;
     u64* const box1 = box0 + kBoxWords;
     const long long jobs = (long long)q.B * q.H * q.chunks * q.nt;
@@ -207,41 +315,60 @@ __global__ __launch_bounds__(kThreads) void k_chunk_out(ChunkArgs q)
         const long long at = bh * q.T + t0;
         u64 z0[8] = {}, z1[8] = {};
         Unit u;
+        if (left) {                                               // W: nothing above the diagonal
+            const long long o = at * kChunk;
+            fetch<true>(u.own0, q.w_x0 + o, kChunk, L, kChunk);
+            fetch<true>(u.open, q.w_open + o, kChunk, L, kChunk);
+            fetch<true>(u.mask1, q.a_w[1] + o, kChunk, L, kChunk);
 #pragma unroll
-        for (int k = 0; k < kUnit; ++k) {
-            const int j = kb * kUnit + k, d = n0 + row;
-            u.own0[k] = u.open[k] = u.mask1[k] = 0;
-            if (left ? row < L && j <= row : j < L && d < q.dv) {
-                if (left) {
-                    const long long o = (at + row) * kChunk + j;
-                    u.own0[k] = q.w_x0[o]; u.open[k] = q.w_open[o]; u.mask1[k] = q.a_w[1][o];
-                } else {
-                    const long long o = b * q.v.b + h * q.v.h + (t0 + j) * q.v.t + d, oa = (at + j) * q.dv + d;
-                    u.mask1[k] = q.a_v[1][oa];
-                    u.own0[k] = q.v.p[0][o] + q.recv_v[0][oa];
-                    u.open[k] = q.v.p[1][o] - u.mask1[k] + q.recv_v[1][oa];
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int row = Place<true>::row(i);
+                    if (row >= L || Place<true>::k(i) + j > row) u.own0[i][j] = u.open[i][j] = u.mask1[i][j] = 0;
                 }
-            }
+        } else {
+            const long long o = b * q.v.b + h * q.v.h + t0 * q.v.t + n0, oa = at * q.dv + n0;
+            const int cols = q.dv - n0;
+            Words r0, r1;
+            fetch<false>(u.own0, q.v.p[0] + o, q.v.t, cols, L);
+            fetch<false>(u.open, q.v.p[1] + o, q.v.t, cols, L);
+            fetch<false>(u.mask1, q.a_v[1] + oa, q.dv, cols, L);
+            fetch<false>(r0, q.recv_v[0] + oa, q.dv, cols, L);
+            fetch<false>(r1, q.recv_v[1] + oa, q.dv, cols, L);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const bool in = there<false>(i, j, cols, L);
+                    u.own0[i][j] = in ? u.own0[i][j] + r0[i][j] : 0;
+                    u.open[i][j] = in ? u.open[i][j] - u.mask1[i][j] + r1[i][j] : 0;
+                    if (!in) u.mask1[i][j] = 0;
+                }
         }
-        multiply_unit(s, u, z0, z1);
+        multiply_unit<true, false>(lds, u, z0, z1);
         for (int k0 = 0; k0 < q.dk; k0 += 64) {
-            const int k = k0 + kb * kUnit, n = q.dk - k;
             if (left) {
-                const long long o = b * q.q.b + h * q.q.h + (t0 + row) * q.q.t + k, oa = (at + row) * q.dk + k;
-                const u64 f = row < L ? (u64)(int64_t)pow[row + 1] : 0;
-                open_unit<true>(u, q.q.p[0] + o, q.q.p[1] + o, 1, q.a_qd[0] + oa, q.a_qd[1] + oa, 1, row < L ? n : 0, [&](int) { return f; },
-                                q.bits, n0 == 0 ? box0 : nullptr, box1, kThreads);
+                const long long o = b * q.q.b + h * q.q.h + t0 * q.q.t + k0, oa = at * q.dk + k0;
+                open_unit<true, true>(u, q.q.p[0] + o, q.q.p[1] + o, q.q.t, q.a_qd[0] + oa, q.a_qd[1] + oa, q.dk, L, q.dk - k0,
+                    [&](int i, int) { const int row = Place<true>::row(i); return (u64)(int64_t)pow[row < L ? row + 1 : 0]; }, q.bits,
+                    [&](int i, int j, u64 to0, u64 to1) {
+                        if (n0) return;
+                        box0[(i * 4 + j) * kThreads] = to0; box1[(i * 4 + j) * kThreads] = to1;
+                    });
             } else {
-                const int d = n0 + row;
+                const long long o = ((bh * q.chunks + chunk) * q.dk + k0) * q.dv + n0;
+                const int cols = q.dv - n0, n = q.dk - k0;
+                fetch<false>(u.own0, q.u[0] + o, q.dv, cols, n);
+                fetch<false>(u.open, q.u[1] + o, q.dv, cols, n);
+                fetch<false>(u.mask1, q.a_s[1] + o, q.dv, cols, n);
 #pragma unroll
-                for (int i = 0; i < kUnit; ++i) {
-                    u.own0[i] = u.open[i] = u.mask1[i] = 0;
-                    if (d >= q.dv || i >= n) continue;
-                    const long long o = ((bh * q.chunks + chunk) * q.dk + k + i) * q.dv + d;
-                    u.own0[i] = q.u[0][o]; u.open[i] = q.u[1][o]; u.mask1[i] = q.a_s[1][o];
-                }
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (!there<false>(i, j, cols, n)) u.own0[i][j] = u.open[i][j] = u.mask1[i][j] = 0;
             }
-            multiply_unit(s, u, z0, z1);
+            multiply_unit<true, false>(lds, u, z0, z1);
         }
         each_word([&](int r, int i, int j) {
             if (i >= L || n0 + j >= q.dv) return;
@@ -326,6 +453,7 @@ __global__ __launch_bounds__(256) void k_step(StepArgs q)
 }
 
 bool strides_in(const mpc_strides& s) { return s.batch >= 0 && s.token >= 0 && s.head >= 0; }
+bool far_tokens(const mpc_strides& s) { return s.token > kMaxStride; }
 
 // words from the first to the last one of [B][T][H][d] with these strides
 size_t extent(const mpc_strides& s, int B, int T, int H, int d)
@@ -397,6 +525,7 @@ int mpc_linear_attention(mpc_ctx* c, mpc_cshare q, mpc_cshare k, mpc_cshare v, m
     for (const mpc_cshare* x : mats) if (!both(*x)) return MPC_EINVAL;
     MPC_TRY(shape_ok(c, B, T, H, dk, dv));
     if (!strides_in(sq) || !strides_in(sk) || !strides_in(sv) || !strides_out(so, B, T, H, dv)) return MPC_EINVAL;
+    if (far_tokens(sq) || far_tokens(sk) || far_tokens(sv)) return MPC_ERANGE;
     const ChunkPlan p = plan(B, T, H, dk, dv);
     const size_t n_o = extent(so, B, T, H, dv) * 8, n_s = (size_t)B * H * dk * dv * 8;
     const size_t BHT = (size_t)B * H * T * 8;
@@ -430,9 +559,9 @@ int mpc_linear_attention(mpc_ctx* c, mpc_cshare q, mpc_cshare k, mpc_cshare v, m
     const auto grid = [](long long jobs, long long most) { return dim3((unsigned)(jobs < most ? jobs : most)); };
     const long long cells = (long long)B * H * p.chunks;
     MPC_TRY(lane_first(c));
-    k_chunk_open<<<grid(cells * (1 + a.mt * a.nt), kBoxes), kThreads, 0, c->s[0]>>>(a);
+    k_chunk_open<<<grid(cells * (1 + a.mt * a.nt), kBoxes), kThreads, 4 * kOperand, c->s[0]>>>(a);
     k_chunk_states<<<grid(((long long)n_s / 8 + 255) / 256, 4096), 256, 0, c->s[0]>>>(a);
-    k_chunk_out<<<grid(cells * a.nt, kBoxes), kThreads, 0, c->s[0]>>>(a);
+    k_chunk_out<<<grid(cells * a.nt, kBoxes), kThreads, 4 * kOperand, c->s[0]>>>(a);
     MPC_HIP(c, hipGetLastError());
     return lane_fanout(c);
 }
