@@ -4,10 +4,16 @@
 
 typedef u64 u64x2u __attribute__((ext_vector_type(2), aligned(8)));   // two words at any word's address
 
-// one party's side of the local rescale; bits = 0 leaves the word as it is
+// z >> bits for bits in [0, 31], in two single-width instructions
+__device__ __forceinline__ u64 shifted(u64 z, int bits)
+{
+    const uint32_t lo = (uint32_t)z, hi = (uint32_t)(z >> 32);
+    return (u64)(hi >> bits) << 32 | __builtin_amdgcn_alignbit(hi, lo, bits);
+}
+// one party's side of the local rescale by 0 to 31 bits; none leaves the word as it is
 template <int PARTY> __device__ __forceinline__ u64 rescaled(u64 z, int bits)
 {
-    return PARTY == 0 ? z >> bits : (u64)0 - (((u64)0 - z) >> bits);
+    return PARTY == 0 ? shifted(z, bits) : (u64)0 - shifted((u64)0 - z, bits);
 }
 __device__ __forceinline__ u64 rescaled(int party, u64 z, int bits) { return party == 0 ? rescaled<0>(z, bits) : rescaled<1>(z, bits); }
 

@@ -20,10 +20,10 @@ namespace {
 
 constexpr int kChunk = MPC_ATTENTION_CHUNK;   // 64
 constexpr int kThreads = 512;
-constexpr int kUnit = 16;                     // words along the contraction that a thread brings
-constexpr int kBoxes = 512;                   // workgroups of a launch, each with receive buffers of its own
+constexpr int kBoxes = 256;                   // workgroups of a launch, one to a compute unit, each with receive buffers of its own
+constexpr int kStateBoxes = 2048;             // workgroups of the states' launch, eight to a compute unit: 512 words each
 constexpr long long kMaxStride = MPC_ATTENTION_MAX_TOKEN_STRIDE;   // 64 tokens stay below 2^31 bytes
-constexpr size_t kBoxWords = (size_t)kThreads * kUnit;   // per direction
+constexpr size_t kBoxWords = (size_t)kThreads * 4;   // per direction
 
 struct Rows { const u64* p[2]; long long b, t, h; };     // words of (batch, token, head) at p + b*b + t*t + h*h
 
@@ -41,100 +41,119 @@ struct ChunkArgs {
     int mt, nt;                               // tiles of 64 along dk and dv
 };
 
-// A thread brings 16 words of an operand tile of 64 rows by 64 along the contraction, as four quads along the contraction: of
-// four rows where a row's words are adjacent in memory (four lanes read 128 bytes), else of one row, neighbouring lanes on
-// neighbouring rows.  The first four waves bring the left operand, the others the right one.
-__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64)); }
-template <bool ADJACENT> struct Place {
-    __device__ __forceinline__ static int row(int i) { const int l = threadIdx.x % 64; return ADJACENT ? i * 16 + l / 4 : l; }
-    __device__ __forceinline__ static int k(int i) { return wave_id() % 4 * 16 + (ADJACENT ? (int)threadIdx.x % 4 : i) * 4; }
-};
-typedef u64 Words[4][4];
-
-__device__ __forceinline__ u64 word_at(const u64* base, unsigned bytes) { return *reinterpret_cast<const u64*>(reinterpret_cast<const u8*>(base) + bytes); }
-
-// Word (row, k) lies at base + row*rs + k*ks, one of the two strides being 1.  Rows and columns that are not there repeat the
-// last one (its value is not used).  Offsets from the tile's first word are below 2^31 bytes (kMaxStride).
-template <bool ADJACENT>
-__device__ __forceinline__ void fetch(Words& w, const u64* base, long long stride, int rows, int cols, int from = 0, int to = 4)
-{
-#pragma unroll
-    for (int i = from; i < to; ++i) {
-        const int row = Place<ADJACENT>::row(i), k = Place<ADJACENT>::k(i);
-        const unsigned r = row < rows ? row : rows - 1;
-        if (ADJACENT) {
-            const unsigned off = r * ((unsigned)stride * 8);
-            if (cols % 4 == 0) {
-                const u8* const at = reinterpret_cast<const u8*>(base) + (off + (unsigned)(k < cols ? k : cols - 4) * 8);
-                const u64x2u lo = *reinterpret_cast<const u64x2u*>(at), hi = *reinterpret_cast<const u64x2u*>(at + 16);
-                w[i][0] = lo.x; w[i][1] = lo.y; w[i][2] = hi.x; w[i][3] = hi.y;
-            } else
-#pragma unroll
-                for (int j = 0; j < 4; ++j) w[i][j] = word_at(base, off + (unsigned)(k + j < cols ? k + j : cols - 1) * 8);
-        } else
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[i][j] = word_at(base + (k + j < cols ? k + j : cols - 1) * stride, r * 8);
-    }
-}
-template <bool ADJACENT> __device__ __forceinline__ bool there(int i, int j, int rows, int cols)
-{
-    return Place<ADJACENT>::row(i) < rows && Place<ADJACENT>::k(i) + j < cols;
-}
-
-struct Unit { Words own0, open, mask1; };     // party 0's operand x_0 + e_1; e; a_1
-
-// A masked operand; a word's power(i, j) is a public factor, followed by the rescale (DECAY); sent(i, j, to party 0, to party 1).
-template <bool ADJACENT, bool DECAY, class Power, class Sent>
-__device__ __forceinline__ void open_unit(Unit& u, const u64* x0, const u64* x1, long long stride, const u64* a0, const u64* a1,
-                                          long long a_stride, int rows, int cols, Power power, int bits, Sent sent)
-{
-    Words a;                                  // party 0's mask
-#pragma unroll
-    for (int half = 0; half < 4; half += 2) { // two quads in flight: registers
-        fetch<ADJACENT>(u.own0, x0, stride, rows, cols, half, half + 2);
-        fetch<ADJACENT>(u.open, x1, stride, rows, cols, half, half + 2);
-        fetch<ADJACENT>(a, a0, a_stride, rows, cols, half, half + 2);
-        fetch<ADJACENT>(u.mask1, a1, a_stride, rows, cols, half, half + 2);
-#pragma unroll
-        for (int i = half; i < half + 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                u64 w0 = u.own0[i][j], w1 = u.open[i][j];
-                if (DECAY) { const u64 f = power(i, j); w0 = rescaled<0>(w0 * f, bits); w1 = rescaled<1>(w1 * f, bits); }
-                const bool in = there<ADJACENT>(i, j, rows, cols);
-                const u64 e0 = w0 - a[i][j], e1 = w1 - u.mask1[i][j];
-                if (in) sent(i, j, e1, e0);
-                u.own0[i][j] = in ? w0 + e1 : 0; u.open[i][j] = in ? e0 + e1 : 0; if (!in) u.mask1[i][j] = 0;
-            }
-        __builtin_amdgcn_sched_barrier(0);
-    }
-}
-
-// ---- products of 64 x 64 x 64 words on the matrix cores: eight digit planes of an operand tile in LDS, [digit][k/16][row][16]
+// Products of 64 x 64 x 64 words run on the matrix cores, from eight digit planes of each operand tile in LDS,
+// [digit][k/16][row][16]; five operand tiles fill the 160 KB of a compute unit.
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 constexpr int kPlane = 64 * 64, kOperand = 8 * kPlane;      // bytes
+enum { kOwnLeft, kOwnRight, kOpenLeft, kMaskRight, kOpenRight, kOperands, kMaskLeft = kOwnLeft };
 
-template <bool ADJACENT> __device__ __forceinline__ void stage(u8* to, const Words& w)
+// The first four waves bring the left operand, the others the right one: 16 words a thread, as four quads of rows 16 apart.
+// Wave w of the four has words 16w..16w+15 of the contraction; quad kq of them is {2kq, 2kq+1, 8+2kq, 9+2kq}, in the same order
+// for both operands, since a product does not care which.  Where a row's words are adjacent in memory (ADJACENT), four lanes read
+// 64 bytes of a row at once; else sixteen lanes read 128 bytes across the rows.  Stores to LDS meet every bank once either way.
+struct Place { int wave, lane; };             // wave: the same for all lanes, read once (a scalar)
+__device__ __forceinline__ Place place() { return Place{ __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64)), (int)threadIdx.x % 64 }; }
+
+struct Quad { u64 w[4]; };
+
+// A tile of `rows` rows and `cols` words along the contraction, at most 64 each of what is there; word (row, k) lies at
+// p + row*rs + k*ks words, one of the strides being 1 (ADJACENT: ks).  Rows and columns that are not there repeat the last one.
+// Offsets within a tile are below 2^31 bytes (kMaxStride).
+template <bool ADJACENT> struct Tile {
+    int rows, cols, row0, k0, quad;
+    __device__ __forceinline__ Tile(const Place& p, int rows_, int cols_)
+        : rows(rows_), cols(cols_), row0(ADJACENT ? p.lane / 4 : p.lane % 16), quad(ADJACENT ? p.lane % 4 : p.lane / 16) { k0 = p.wave % 4 * 16 + quad * 2; }
+    __device__ __forceinline__ int row(int i) const { return row0 + i * 16; }
+    __device__ __forceinline__ int k(int j) const { return k0 + j % 2 + j / 2 * 8; }
+    __device__ __forceinline__ Quad load(const u64* p, long long stride, int i) const
+    {
+        const u8* const base = reinterpret_cast<const u8*>(p);
+        const unsigned r = min(row(i), rows - 1), s = (unsigned)stride * 8;
+        Quad q;
+        if (ADJACENT && cols % 2 == 0) {
+#pragma unroll
+            for (int j = 0; j < 4; j += 2) {
+                const u64x2u w = *reinterpret_cast<const u64x2u*>(base + (r * s + min(k(j), cols - 2) * 8u));
+                q.w[j] = w.x; q.w[j + 1] = w.y;
+            }
+        } else
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const unsigned c = min(k(j), cols - 1);
+                q.w[j] = *reinterpret_cast<const u64*>(base + (ADJACENT ? r * s + c * 8 : c * s + r * 8));
+            }
+        return q;
+    }
+    __device__ __forceinline__ bool has(int i, int j) const { return row(i) < rows && k(j) < cols; }
+    __device__ __forceinline__ void clear(int i, Quad& q) const
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) q.w[j] = has(i, j) ? q.w[j] : 0;
+    }
+    __device__ __forceinline__ void stage(u8* lds, int operand, int i, const Quad& q) const
+    {
+        uint32_t d[8];
+        digits_of_4(q.w, d);
+        u8* const at = lds + operand * kOperand + k0 / 16 * 1024 + (row(i) * 16 + quad * 4);
+#pragma unroll
+        for (int p = 0; p < 8; ++p) *reinterpret_cast<uint32_t*>(at + p * kPlane) = d[p];
+    }
+};
+
+// A thread's quads of an operand: load(i) asks for words, form(i, words, own0, open, mask1) makes party 0's operand x_0 + e_1, the
+// opened words and party 1's mask of them.  All words are asked for at once, ahead of the barrier behind which the last products'
+// operands may be written over: one after the other their latency was most of a job's time.
+template <bool LEFT, bool ADJACENT, class Load, class Form> __device__ __forceinline__ void bring(u8* lds, const Tile<ADJACENT>& t, Load load, Form form)
 {
-    const int kb = threadIdx.x / 64 % 4;
-    if (ADJACENT) {
+    const decltype(load(0)) words[4] = { load(0), load(1), load(2), load(3) };
+    __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t d[8];
-            digits_of_4(w[i], d);
-            u8* const at = to + (kb * 64 + Place<true>::row(i)) * 16 + threadIdx.x % 4 * 4;
-#pragma unroll
-            for (int q = 0; q < 8; ++q) *reinterpret_cast<uint32_t*>(at + q * kPlane) = d[q];
-        }
-    } else {
-        uint32_t d[4][8];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) digits_of_4(w[i], d[i]);
-        u8* const at = to + (kb * 64 + threadIdx.x % 64) * 16;
-#pragma unroll
-        for (int q = 0; q < 8; ++q) *reinterpret_cast<uint4*>(at + q * kPlane) = uint4{ d[0][q], d[1][q], d[2][q], d[3][q] };
+    for (int i = 0; i < 4; ++i) {
+        Quad own, open, mask;
+        form(i, words[i], own, open, mask);
+        t.stage(lds, LEFT ? kOwnLeft : kOwnRight, i, own);
+        t.stage(lds, LEFT ? kOpenLeft : kOpenRight, i, open);
+        if (!LEFT) t.stage(lds, kMaskRight, i, mask);
     }
 }
+
+// A masked operand: words of a sharing and of its mask; a word's power(i, j) is a public factor, followed by the rescale (DECAY);
+// sent(i, j, to party 0, to party 1).
+template <bool LEFT, bool ADJACENT, bool DECAY, class Power, class Sent>
+__device__ __forceinline__ void bring_masked(u8* lds, const Tile<ADJACENT>& t, const u64* x0, const u64* x1, long long stride,
+                                             const u64* a0, const u64* a1, long long a_stride, Power power, int bits, Sent sent)
+{
+    struct Raw { Quad x0, x1, a0, a1; };
+    bring<LEFT>(lds, t, [&](int i) { return Raw{ t.load(x0, stride, i), t.load(x1, stride, i), t.load(a0, a_stride, i), t.load(a1, a_stride, i) }; },
+        [&](int i, const Raw& r, Quad& own, Quad& open, Quad& mask) {
+            Quad e0, e1;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                u64 w0 = r.x0.w[j], w1 = r.x1.w[j];
+                if (DECAY) { const u64 f = power(i, j); w0 = rescaled<0>(w0 * f, bits); w1 = rescaled<1>(w1 * f, bits); }
+                e0.w[j] = w0 - r.a0.w[j]; e1.w[j] = w1 - r.a1.w[j];
+                own.w[j] = w0 + e1.w[j]; open.w[j] = e0.w[j] + e1.w[j]; mask.w[j] = r.a1.w[j];
+            }
+            sent(i, e1, e0);
+            t.clear(i, own); t.clear(i, open); t.clear(i, mask);
+        });
+}
+
+// The receive buffers of a workgroup hold what a thread sends at a time, a quad in either direction: they stay in the L2 (with room
+// for a whole tile, 128 KB a workgroup, they were written back to memory, 160 MB a launch of 8 x 512 tokens of 12 heads).
+struct Box {
+    u64 *to0, *to1;
+    __device__ __forceinline__ Box(u64* box) : to0(box + blockIdx.x * 2 * kBoxWords + threadIdx.x * 2), to1(to0 + kBoxWords) {}
+    __device__ __forceinline__ void put(const Quad& e1, const Quad& e0) const
+    {
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) {
+            *reinterpret_cast<u64x2u*>(to0 + j * kThreads) = u64x2u{ e1.w[j], e1.w[j + 1] };
+            *reinterpret_cast<u64x2u*>(to1 + j * kThreads) = u64x2u{ e0.w[j], e0.w[j + 1] };
+        }
+    }
+    __device__ __forceinline__ void put(int r, u64 e1, u64 e0) const { to0[r % 2 + r / 2 % 2 * 2 * kThreads] = e1; to1[r % 2 + r / 2 % 2 * 2 * kThreads] = e0; }
+};
 
 // A wave has 16 rows and two tiles of 16 columns; acc[tile][s] sums the products of digits i + j = s.  One K step of 64 adds at
 // most (s + 1) 2^20 to it.
@@ -146,11 +165,11 @@ __device__ __forceinline__ void clear(Sums& z)
 #pragma unroll
         for (int s = 0; s < 8; ++s) z.s[t][s] = i32x4{ 0, 0, 0, 0 };
 }
-__device__ __forceinline__ void multiply(const u8* lds, Sums& z)
+__device__ __forceinline__ void multiply(const u8* lds, const Place& p, int left, int right, Sums& z)
 {
-    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
-    const u8* const l = lds + (lane / 16 * 64 + wave % 4 * 16 + lane % 16) * 16;
-    const u8* const r = lds + kOperand + (lane / 16 * 64 + wave / 4 * 32 + lane % 16) * 16;
+    const int wave = p.wave, lane = p.lane;
+    const u8* const l = lds + left * kOperand + (lane / 16 * 64 + wave % 4 * 16 + lane % 16) * 16;
+    const u8* const r = lds + right * kOperand + (lane / 16 * 64 + wave / 4 * 32 + lane % 16) * 16;
     i32x4 a[8];
 #pragma unroll
     for (int d = 0; d < 8; ++d) a[d] = *reinterpret_cast<const i32x4*>(l + d * kPlane);
@@ -182,96 +201,106 @@ __device__ __forceinline__ void join(const Sums& a, u64 (&z)[8])
         }
 }
 
-// z0 += own0 own0', z1 += open mask1' + mask1 open'.  The first two products' operands are in LDS together; the third's take
-// the first one's place.
-template <bool LEFT_ADJACENT, bool RIGHT_ADJACENT>
-__device__ __forceinline__ void multiply_unit(u8* lds, const Unit& u, u64 (&z0)[8], u64 (&z1)[8])
+// z0 += own0 own0', z1 += open mask1' + mask1 open' once both operands are in LDS.  Party 1's mask of the left operand, mask(i),
+// is asked for under the first two products and takes the place of party 0's operand: all waves bring it, two quads each.
+template <bool ADJACENT, class Mask> __device__ __forceinline__ void multiply_all(u8* lds, const Place& p, const Tile<ADJACENT>& t, Mask mask, u64 (&z0)[8], u64 (&z1)[8])
 {
-    __syncthreads();
-    if (wave_id() < 4) { stage<LEFT_ADJACENT>(lds, u.own0); stage<LEFT_ADJACENT>(lds + 2 * kOperand, u.open); }
-    else { stage<RIGHT_ADJACENT>(lds + kOperand, u.own0); stage<RIGHT_ADJACENT>(lds + 3 * kOperand, u.mask1); }
-    __syncthreads();
+    const int first = p.wave / 4 * 2;
     Sums a;
     clear(a);
-    multiply(lds, a);
+    const Quad m0 = mask(first), m1 = mask(first + 1);
+    __syncthreads();
+    multiply(lds, p, kOwnLeft, kOwnRight, a);
     join(a, z0);
-    __syncthreads();
-    if (wave_id() < 4) stage<LEFT_ADJACENT>(lds, u.mask1); else stage<RIGHT_ADJACENT>(lds + kOperand, u.open);
     clear(a);
-    multiply(lds + 2 * kOperand, a);
+    multiply(lds, p, kOpenLeft, kMaskRight, a);
     __syncthreads();
-    multiply(lds, a);
+    t.stage(lds, kMaskLeft, first, m0);
+    t.stage(lds, kMaskLeft, first + 1, m1);
+    __syncthreads();
+    multiply(lds, p, kMaskLeft, kOpenRight, a);
     join(a, z1);
 }
 // each(index, row, column) of a thread's words of the product
-template <class Each> __device__ __forceinline__ void each_word(Each each)
+template <class Each> __device__ __forceinline__ void each_word(const Place& p, Each each)
 {
-    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
 #pragma unroll
-    for (int r = 0; r < 8; ++r) each(r, wave % 4 * 16 + lane / 16 * 4 + r % 4, wave / 4 * 32 + r / 4 * 16 + lane % 16);
+    for (int r = 0; r < 8; ++r) each(r, p.wave % 4 * 16 + p.lane / 16 * 4 + r % 4, p.wave / 4 * 32 + r / 4 * 16 + p.lane % 16);
 }
 
-struct NoPower { __device__ u64 operator()(int, int) const { return 1; } };
+struct NoPower { __device__ uint32_t operator()(int, int) const { return 1; } };
 
 // P and W of a chunk, or one tile of its U.
 __global__ __launch_bounds__(kThreads) void k_chunk_open(ChunkArgs q)
 {
-    extern __shared__ __attribute__((aligned(16))) u8 lds[];          // 4 kOperand
-    const bool left = wave_id() < 4;
-    u64* const box0 = q.box + blockIdx.x * 2 * kBoxWords + threadIdx.x;
-    u64* const box1 = box0 + kBoxWords;
-    const auto to_box = [&](int i, int j, u64 to0, u64 to1) { box0[(i * 4 + j) * kThreads] = to0; box1[(i * 4 + j) * kThreads] = to1; };
-    const long long jobs = (long long)q.B * q.H * q.chunks * (1 + q.mt * q.nt);
-    for (long long job = blockIdx.x; job < jobs; job += gridDim.x) {
-        const int kind = (int)(job % (1 + q.mt * q.nt));
-        const int chunk = (int)(job / (1 + q.mt * q.nt) % q.chunks);
-        const long long bh = job / (1 + q.mt * q.nt) / q.chunks;
-        const int b = (int)(bh / q.H), h = (int)(bh % q.H), t0 = chunk * kChunk, L = q.T - t0 < kChunk ? q.T - t0 : kChunk;
+    extern __shared__ __attribute__((aligned(16))) u8 lds[];          // kOperands kOperand
+    const Place p = place();
+    const bool left = p.wave < 4;
+    const Box box(q.box);
+    const auto to_box = [&](int, const Quad& e1, const Quad& e0) { box.put(e1, e0); };
+    const unsigned kinds = 1 + q.mt * q.nt, jobs = (unsigned)q.B * q.H * q.chunks * kinds;
+    for (unsigned job = blockIdx.x; job < jobs; job += gridDim.x) {
+        const int kind = job % kinds, chunk = job / kinds % q.chunks;
+        const long long bh = job / kinds / q.chunks;
+        const int b = (int)bh / q.H, h = (int)bh % q.H, t0 = chunk * kChunk, L = q.T - t0 < kChunk ? q.T - t0 : kChunk;
         const int32_t* const pow = q.decay + h * (kChunk + 1);
         const long long at = bh * q.T + t0;                       // the chunk's first token in the dense arrays
+        const long long ok = b * q.k.b + h * q.k.h + t0 * q.k.t;
         u64 z0[8] = {}, z1[8] = {};
         if (kind == 0) {
-            const Rows& x = left ? q.q : q.k;
-            const u64* const* a = left ? q.a_q : q.a_k;
+            const long long oq = b * q.q.b + h * q.q.h + t0 * q.q.t;
             for (int k0 = 0; k0 < q.dk; k0 += 64) {
-                const long long o = b * x.b + h * x.h + t0 * x.t + k0, oa = at * q.dk + k0;
-                Unit u;
-                open_unit<true, false>(u, x.p[0] + o, x.p[1] + o, x.t, a[0] + oa, a[1] + oa, q.dk, L, q.dk - k0, NoPower{}, 0, to_box);
-                multiply_unit<true, true>(lds, u, z0, z1);
+                const Tile<true> t(p, L, q.dk - k0);
+                const long long oa = at * q.dk + k0;
+                if (left) bring_masked<true, true, false>(lds, t, q.q.p[0] + oq + k0, q.q.p[1] + oq + k0, q.q.t, q.a_q[0] + oa, q.a_q[1] + oa, q.dk, NoPower{}, 0, to_box);
+                else bring_masked<false, true, false>(lds, t, q.k.p[0] + ok + k0, q.k.p[1] + ok + k0, q.k.t, q.a_k[0] + oa, q.a_k[1] + oa, q.dk, NoPower{}, 0, to_box);
+                multiply_all(lds, p, t, [&](int i) { Quad m = t.load(q.a_q[1] + oa, q.dk, i); t.clear(i, m); return m; }, z0, z1);
             }
-            each_word([&](int r, int i, int j) {
+            u64 c0[8], c1[8], a0[8], a1[8], f[8];                  // all asked for together
+            each_word(p, [&](int r, int i, int j) {
+                const bool in = i < L && j <= i;
+                const long long o = in ? (at + i) * kChunk + j : at * kChunk;
+                c0[r] = q.c_p[0][o]; c1[r] = q.c_p[1][o]; a0[r] = q.a_w[0][o]; a1[r] = q.a_w[1][o]; f[r] = (uint32_t)pow[in ? i - j : 0];
+            });
+            each_word(p, [&](int r, int i, int j) {
                 if (i >= L || j > i) return;
                 const long long o = (at + i) * kChunk + j;
-                const u64 f = (u64)(int64_t)pow[i - j];
-                const u64 w0 = rescaled<0>(rescaled<0>(q.c_p[0][o] + z0[r], q.bits) * f, q.bits);
-                const u64 w1 = rescaled<1>(rescaled<1>(q.c_p[1][o] + z1[r], q.bits) * f, q.bits);
-                const u64 e0 = w0 - q.a_w[0][o], e1 = w1 - q.a_w[1][o];
-                box0[r * kThreads] = e1; box1[r * kThreads] = e0;
+                const u64 w0 = rescaled<0>(rescaled<0>(c0[r] + z0[r], q.bits) * f[r], q.bits);
+                const u64 w1 = rescaled<1>(rescaled<1>(c1[r] + z1[r], q.bits) * f[r], q.bits);
+                const u64 e0 = w0 - a0[r], e1 = w1 - a1[r];
+                box.put(r, e1, e0);
                 q.w_x0[o] = w0 + e1; q.w_open[o] = e0 + e1;
             });
         } else {
             const int m0 = (kind - 1) / q.nt * 64, n0 = (kind - 1) % q.nt * 64;      // contraction over the chunk's tokens
-            Unit u;
-            if (left) {
-                const long long o = b * q.k.b + h * q.k.h + t0 * q.k.t + m0, oa = at * q.dk + m0;
-                open_unit<false, true>(u, q.k.p[0] + o, q.k.p[1] + o, q.k.t, q.a_kd[0] + oa, q.a_kd[1] + oa, q.dk, q.dk - m0, L,
-                    [&](int i, int j) { const int k = Place<false>::k(i) + j; return (u64)(int64_t)pow[k < L ? L - 1 - k : 0]; }, q.bits,
-                    [&](int i, int j, u64 to0, u64 to1) { if (n0 == 0) to_box(i, j, to0, to1); });
-            } else {
-                const long long o = b * q.v.b + h * q.v.h + t0 * q.v.t + n0, oa = at * q.dv + n0;
-                open_unit<false, false>(u, q.v.p[0] + o, q.v.p[1] + o, q.v.t, q.a_v[0] + oa, q.a_v[1] + oa, q.dv, q.dv - n0, L, NoPower{}, 0,
-                    [&](int i, int j, u64 to0, u64 to1) {
+            const Tile<false> tk(p, q.dk - m0, L), tv(p, q.dv - n0, L);
+            const long long oa = at * q.dk + m0, ov = b * q.v.b + h * q.v.h + t0 * q.v.t + n0, oav = at * q.dv + n0;
+            if (left) bring_masked<true, false, true>(lds, tk, q.k.p[0] + ok + m0, q.k.p[1] + ok + m0, q.k.t, q.a_kd[0] + oa, q.a_kd[1] + oa, q.dk,
+                    [&](int, int j) { const int k = tk.k(j); return (uint32_t)pow[k < L ? L - 1 - k : 0]; }, q.bits,
+                    [&](int, const Quad& e1, const Quad& e0) { if (n0 == 0) box.put(e1, e0); });
+            else bring_masked<false, false, false>(lds, tv, q.v.p[0] + ov, q.v.p[1] + ov, q.v.t, q.a_v[0] + oav, q.a_v[1] + oav, q.dv, NoPower{}, 0,
+                    [&](int i, const Quad& e1, const Quad& e0) {
                         if (m0) return;
-                        const long long to = oa + Place<false>::row(i) + (long long)(Place<false>::k(i) + j) * q.dv;
-                        q.recv_v[0][to] = to0; q.recv_v[1][to] = to1;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            if (!tv.has(i, j)) continue;
+                            const long long to = oav + tv.row(i) + tv.k(j) * q.dv;
+                            q.recv_v[0][to] = e1.w[j]; q.recv_v[1][to] = e0.w[j];
+                        }
                     });
-            }
-            multiply_unit<false, false>(lds, u, z0, z1);
-            each_word([&](int r, int i, int jj) {
+            multiply_all(lds, p, tk, [&](int i) { Quad m = tk.load(q.a_kd[1] + oa, q.dk, i); tk.clear(i, m); return m; }, z0, z1);
+            const long long cell = (bh * q.chunks + chunk) * q.dk * q.dv;
+            u64 c0[8], c1[8];
+            each_word(p, [&](int r, int i, int jj) {
+                const int d = m0 + i, e = n0 + jj;
+                const long long o = cell + (d < q.dk && e < q.dv ? d * q.dv + e : 0);
+                c0[r] = q.c_u[0][o]; c1[r] = q.c_u[1][o];
+            });
+            each_word(p, [&](int r, int i, int jj) {
                 const int d = m0 + i, e = n0 + jj;
                 if (d >= q.dk || e >= q.dv) return;
-                const long long o = ((bh * q.chunks + chunk) * q.dk + d) * q.dv + e;
-                q.u[0][o] = q.c_u[0][o] + z0[r]; q.u[1][o] = q.c_u[1][o] + z1[r];
+                const long long o = cell + d * q.dv + e;
+                q.u[0][o] = c0[r] + z0[r]; q.u[1][o] = c1[r] + z1[r];
             });
         }
     }
@@ -292,7 +321,7 @@ __global__ __launch_bounds__(256) void k_chunk_states(ChunkArgs q)
             box0[0] = e1; box0[256] = e0;
             q.u[0][o] = s0 + e1; q.u[1][o] = e0 + e1;
             const int L = q.T - c * kChunk < kChunk ? q.T - c * kChunk : kChunk;
-            const u64 f = (u64)(int64_t)pow[L];
+            const u64 f = (uint32_t)pow[L];
             s0 = rescaled<0>(s0 * f + u0, q.bits); s1 = rescaled<1>(s1 * f + u1, q.bits);
         }
         if (q.state_out[0]) { q.state_out[0][e] = s0; q.state_out[1][e] = s1; }
@@ -302,79 +331,72 @@ __global__ __launch_bounds__(256) void k_chunk_states(ChunkArgs q)
 // O of a chunk, 64 columns of dv: first the part within the chunk, then the state's.
 __global__ __launch_bounds__(kThreads) void k_chunk_out(ChunkArgs q)
 {
-    extern __shared__ __attribute__((aligned(16))) u8 lds[];          // 4 kOperand
-    const bool left = wave_id() < 4;
-    u64* const box0 = q.box + blockIdx.x * 2 * kBoxWords + threadIdx.x;
-    u64* const box1 = box0 + kBoxWords;
-    const long long jobs = (long long)q.B * q.H * q.chunks * q.nt;
-    for (long long job = blockIdx.x; job < jobs; job += gridDim.x) {
-        const int n0 = (int)(job % q.nt) * 64, chunk = (int)(job / q.nt % q.chunks);
+    extern __shared__ __attribute__((aligned(16))) u8 lds[];          // kOperands kOperand
+    const Place p = place();
+    const bool left = p.wave < 4;
+    const Box box(q.box);
+    const unsigned jobs = (unsigned)q.B * q.H * q.chunks * q.nt;
+    struct Three { Quad own, open, mask; };
+    for (unsigned job = blockIdx.x; job < jobs; job += gridDim.x) {
+        const int n0 = (int)(job % q.nt) * 64, chunk = job / q.nt % q.chunks;
         const long long bh = job / q.nt / q.chunks;
-        const int b = (int)(bh / q.H), h = (int)(bh % q.H), t0 = chunk * kChunk, L = q.T - t0 < kChunk ? q.T - t0 : kChunk;
+        const int b = (int)bh / q.H, h = (int)bh % q.H, t0 = chunk * kChunk, L = q.T - t0 < kChunk ? q.T - t0 : kChunk;
         const int32_t* const pow = q.decay + h * (kChunk + 1);
-        const long long at = bh * q.T + t0;
+        const long long at = bh * q.T + t0, ow = at * kChunk;
         u64 z0[8] = {}, z1[8] = {};
-        Unit u;
-        if (left) {                                               // W: nothing above the diagonal
-            const long long o = at * kChunk;
-            fetch<true>(u.own0, q.w_x0 + o, kChunk, L, kChunk);
-            fetch<true>(u.open, q.w_open + o, kChunk, L, kChunk);
-            fetch<true>(u.mask1, q.a_w[1] + o, kChunk, L, kChunk);
+        const Tile<true> tw(p, L, kChunk);
+        const auto below = [&](int i, Quad& w) {                  // W: nothing above the diagonal
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int row = Place<true>::row(i);
-                    if (row >= L || Place<true>::k(i) + j > row) u.own0[i][j] = u.open[i][j] = u.mask1[i][j] = 0;
-                }
-        } else {
+            for (int j = 0; j < 4; ++j) {
+                const u64 keep = -(u64)(tw.row(i) < L && tw.k(j) <= tw.row(i));
+                w.w[j] &= keep;
+            }
+        };
+        if (left) bring<true>(lds, tw, [&](int i) { return Three{ tw.load(q.w_x0 + ow, kChunk, i), tw.load(q.w_open + ow, kChunk, i), {} }; },
+                [&](int i, const Three& r, Quad& own, Quad& open, Quad&) { own = r.own; open = r.open; below(i, own); below(i, open); });
+        else {
             const long long o = b * q.v.b + h * q.v.h + t0 * q.v.t + n0, oa = at * q.dv + n0;
-            const int cols = q.dv - n0;
-            Words r0, r1;
-            fetch<false>(u.own0, q.v.p[0] + o, q.v.t, cols, L);
-            fetch<false>(u.open, q.v.p[1] + o, q.v.t, cols, L);
-            fetch<false>(u.mask1, q.a_v[1] + oa, q.dv, cols, L);
-            fetch<false>(r0, q.recv_v[0] + oa, q.dv, cols, L);
-            fetch<false>(r1, q.recv_v[1] + oa, q.dv, cols, L);
+            const Tile<false> t(p, q.dv - n0, L);
+            struct Raw { Quad v0, v1, a1, r0, r1; };
+            bring<false>(lds, t, [&](int i) { return Raw{ t.load(q.v.p[0] + o, q.v.t, i), t.load(q.v.p[1] + o, q.v.t, i), t.load(q.a_v[1] + oa, q.dv, i),
+                                                       t.load(q.recv_v[0] + oa, q.dv, i), t.load(q.recv_v[1] + oa, q.dv, i) }; },
+                [&](int i, const Raw& r, Quad& own, Quad& open, Quad& mask) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const bool in = there<false>(i, j, cols, L);
-                    u.own0[i][j] = in ? u.own0[i][j] + r0[i][j] : 0;
-                    u.open[i][j] = in ? u.open[i][j] - u.mask1[i][j] + r1[i][j] : 0;
-                    if (!in) u.mask1[i][j] = 0;
-                }
+                    for (int j = 0; j < 4; ++j) { own.w[j] = r.v0.w[j] + r.r0.w[j]; open.w[j] = r.v1.w[j] - r.a1.w[j] + r.r1.w[j]; }
+                    mask = r.a1;
+                    t.clear(i, own); t.clear(i, open); t.clear(i, mask);
+                });
         }
-        multiply_unit<true, false>(lds, u, z0, z1);
+        multiply_all(lds, p, tw, [&](int i) { Quad m = tw.load(q.a_w[1] + ow, kChunk, i); below(i, m); return m; }, z0, z1);
         for (int k0 = 0; k0 < q.dk; k0 += 64) {
+            const Tile<true> tq(p, L, q.dk - k0);
+            const long long oa = at * q.dk + k0;
             if (left) {
-                const long long o = b * q.q.b + h * q.q.h + t0 * q.q.t + k0, oa = at * q.dk + k0;
-                open_unit<true, true>(u, q.q.p[0] + o, q.q.p[1] + o, q.q.t, q.a_qd[0] + oa, q.a_qd[1] + oa, q.dk, L, q.dk - k0,
-                    [&](int i, int) { const int row = Place<true>::row(i); return (u64)(int64_t)pow[row < L ? row + 1 : 0]; }, q.bits,
-                    [&](int i, int j, u64 to0, u64 to1) {
-                        if (n0) return;
-                        box0[(i * 4 + j) * kThreads] = to0; box1[(i * 4 + j) * kThreads] = to1;
-                    });
+                const long long o = b * q.q.b + h * q.q.h + t0 * q.q.t + k0;
+                bring_masked<true, true, true>(lds, tq, q.q.p[0] + o, q.q.p[1] + o, q.q.t, q.a_qd[0] + oa, q.a_qd[1] + oa, q.dk,
+                    [&](int i, int) { const int row = tq.row(i); return (uint32_t)pow[row < L ? row + 1 : 0]; }, q.bits,
+                    [&](int, const Quad& e1, const Quad& e0) { if (n0 == 0) box.put(e1, e0); });
             } else {
                 const long long o = ((bh * q.chunks + chunk) * q.dk + k0) * q.dv + n0;
-                const int cols = q.dv - n0, n = q.dk - k0;
-                fetch<false>(u.own0, q.u[0] + o, q.dv, cols, n);
-                fetch<false>(u.open, q.u[1] + o, q.dv, cols, n);
-                fetch<false>(u.mask1, q.a_s[1] + o, q.dv, cols, n);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (!there<false>(i, j, cols, n)) u.own0[i][j] = u.open[i][j] = u.mask1[i][j] = 0;
+                const Tile<false> t(p, q.dv - n0, q.dk - k0);
+                bring<false>(lds, t, [&](int i) { return Three{ t.load(q.u[0] + o, q.dv, i), t.load(q.u[1] + o, q.dv, i), t.load(q.a_s[1] + o, q.dv, i) }; },
+                    [&](int i, const Three& r, Quad& own, Quad& open, Quad& mask) {
+                        own = r.own; open = r.open; mask = r.mask;
+                        t.clear(i, own); t.clear(i, open); t.clear(i, mask);
+                    });
             }
-            multiply_unit<true, false>(lds, u, z0, z1);
+            multiply_all(lds, p, tq, [&](int i) { Quad m = tq.load(q.a_qd[1] + oa, q.dk, i); tq.clear(i, m); return m; }, z0, z1);
         }
-        each_word([&](int r, int i, int j) {
+        u64 c0[8], c1[8];
+        each_word(p, [&](int r, int i, int j) {
+            const long long o = at * q.dv + (i < L && n0 + j < q.dv ? i * q.dv + n0 + j : 0);
+            c0[r] = q.c_o[0][o]; c1[r] = q.c_o[1][o];
+        });
+        each_word(p, [&](int r, int i, int j) {
             if (i >= L || n0 + j >= q.dv) return;
-            const long long oc = (at + i) * q.dv + n0 + j, o = b * q.ob + h * q.oh + (t0 + i) * q.ot + n0 + j;
-            q.o[0][o] = rescaled<0>(q.c_o[0][oc] + z0[r], q.bits);
-            q.o[1][o] = rescaled<1>(q.c_o[1][oc] + z1[r], q.bits);
+            const long long o = b * q.ob + h * q.oh + (t0 + i) * q.ot + n0 + j;
+            q.o[0][o] = rescaled<0>(c0[r] + z0[r], q.bits);
+            q.o[1][o] = rescaled<1>(c1[r] + z1[r], q.bits);
         });
     }
 }
@@ -405,7 +427,7 @@ __global__ __launch_bounds__(256) void k_step(StepArgs q)
     for (long long job = blockIdx.x; job < jobs; job += gridDim.x) {
         const long long bh = job / q.slices;
         const int slice = (int)(job % q.slices), e = slice * kSlice + col, b = (int)(bh / q.H), h = (int)(bh % q.H);
-        const u64 f = (u64)(int64_t)q.decay[h * (kChunk + 1) + 1];
+        const u64 f = (uint32_t)q.decay[h * (kChunk + 1) + 1];
         {
             const int which = threadIdx.x / kMaxD, d = threadIdx.x % kMaxD;
             const Rows& x = which ? q.q : q.k;
@@ -496,7 +518,7 @@ ChunkPlan plan(int B, int T, int H, int dk, int dv)
     ChunkPlan p{};
     const size_t BH = (size_t)B * H;
     p.chunks = (T + kChunk - 1) / kChunk;
-    p.recv = BH * T * dv; p.w = BH * T * kChunk; p.u = BH * p.chunks * dk * dv; p.box = kBoxes * 2 * kBoxWords;
+    p.recv = BH * T * dv; p.w = BH * T * kChunk; p.u = BH * p.chunks * dk * dv; p.box = kStateBoxes * 512 > kBoxes * 2 * kBoxWords ? kStateBoxes * 512 : kBoxes * 2 * kBoxWords;
     p.total = 2 * align_up(p.recv * 8) + 2 * align_up(p.w * 8) + 2 * align_up(p.u * 8) + align_up(p.box * 8);
     return p;
 }
@@ -527,6 +549,7 @@ int mpc_linear_attention(mpc_ctx* c, mpc_cshare q, mpc_cshare k, mpc_cshare v, m
     if (!strides_in(sq) || !strides_in(sk) || !strides_in(sv) || !strides_out(so, B, T, H, dv)) return MPC_EINVAL;
     if (far_tokens(sq) || far_tokens(sk) || far_tokens(sv)) return MPC_ERANGE;
     const ChunkPlan p = plan(B, T, H, dk, dv);
+    if ((long long)B * H * p.chunks * 5 > INT32_MAX) return MPC_ERANGE;      // jobs of a launch
     const size_t n_o = extent(so, B, T, H, dv) * 8, n_s = (size_t)B * H * dk * dv * 8;
     const size_t BHT = (size_t)B * H * T * 8;
     const size_t sizes[] = { BHT * dk, BHT * dk, BHT * dk, BHT * dk, BHT * dv, BHT * kChunk, p.u * 8, BHT * kChunk, p.u * 8, BHT * dv };
@@ -559,9 +582,9 @@ int mpc_linear_attention(mpc_ctx* c, mpc_cshare q, mpc_cshare k, mpc_cshare v, m
     const auto grid = [](long long jobs, long long most) { return dim3((unsigned)(jobs < most ? jobs : most)); };
     const long long cells = (long long)B * H * p.chunks;
     MPC_TRY(lane_first(c));
-    k_chunk_open<<<grid(cells * (1 + a.mt * a.nt), kBoxes), kThreads, 4 * kOperand, c->s[0]>>>(a);
-    k_chunk_states<<<grid(((long long)n_s / 8 + 255) / 256, 4096), 256, 0, c->s[0]>>>(a);
-    k_chunk_out<<<grid(cells * a.nt, kBoxes), kThreads, 4 * kOperand, c->s[0]>>>(a);
+    k_chunk_open<<<grid(cells * (1 + a.mt * a.nt), kBoxes), kThreads, kOperands * kOperand, c->s[0]>>>(a);
+    k_chunk_states<<<grid(((long long)n_s / 8 + 255) / 256, kStateBoxes), 256, 0, c->s[0]>>>(a);
+    k_chunk_out<<<grid(cells * a.nt, kBoxes), kThreads, kOperands * kOperand, c->s[0]>>>(a);
     MPC_HIP(c, hipGetLastError());
     return lane_fanout(c);
 }
