@@ -39,6 +39,7 @@ struct ChunkArgs {
     u64* box;
     int B, H, T, dk, dv, chunks, bits;
     int mt, nt;                               // tiles of 64 along dk and dv
+    unsigned cells;                           // chunks of all heads
 };
 
 // Products of 64 x 64 x 64 words run on the matrix cores, from eight digit planes of each operand tile in LDS,
@@ -53,6 +54,9 @@ enum { kOwnLeft, kOwnRight, kOpenLeft, kMaskRight, kOpenRight, kOperands, kMaskL
 // 64 bytes of a row at once; else sixteen lanes read 128 bytes across the rows.  Stores to LDS meet every bank once either way.
 struct Place { int wave, lane; };             // wave: the same for all lanes, read once (a scalar)
 __device__ __forceinline__ Place place() { return Place{ __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64)), (int)threadIdx.x % 64 }; }
+// The same place again: offsets and conditions that follow from the lane are made anew, instead of being kept (and spilled) across
+// jobs and steps.
+__device__ __forceinline__ Place anew(Place p) { asm volatile("" : "+v"(p.lane)); return p; }
 
 struct Quad { u64 w[4]; };
 
@@ -123,14 +127,20 @@ template <bool LEFT, bool ADJACENT, bool DECAY, class Power, class Sent>
 __device__ __forceinline__ void bring_masked(u8* lds, const Tile<ADJACENT>& t, const u64* x0, const u64* x1, long long stride,
                                              const u64* a0, const u64* a1, long long a_stride, Power power, int bits, Sent sent)
 {
-    struct Raw { Quad x0, x1, a0, a1; };
-    bring<LEFT>(lds, t, [&](int i) { return Raw{ t.load(x0, stride, i), t.load(x1, stride, i), t.load(a0, a_stride, i), t.load(a1, a_stride, i) }; },
+    struct Raw { Quad x0, x1, a0, a1; uint32_t f[4]; };
+    bring<LEFT>(lds, t, [&](int i) {
+            Raw r{ t.load(x0, stride, i), t.load(x1, stride, i), t.load(a0, a_stride, i), t.load(a1, a_stride, i), {} };
+            if (DECAY)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) r.f[j] = power(i, j);
+            return r;
+        },
         [&](int i, const Raw& r, Quad& own, Quad& open, Quad& mask) {
             Quad e0, e1;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 u64 w0 = r.x0.w[j], w1 = r.x1.w[j];
-                if (DECAY) { const u64 f = power(i, j); w0 = rescaled<0>(w0 * f, bits); w1 = rescaled<1>(w1 * f, bits); }
+                if (DECAY) { w0 = rescaled<0>(w0 * r.f[j], bits); w1 = rescaled<1>(w1 * r.f[j], bits); }
                 e0.w[j] = w0 - r.a0.w[j]; e1.w[j] = w1 - r.a1.w[j];
                 own.w[j] = w0 + e1.w[j]; open.w[j] = e0.w[j] + e1.w[j]; mask.w[j] = r.a1.w[j];
             }
@@ -228,79 +238,94 @@ template <class Each> __device__ __forceinline__ void each_word(const Place& p, 
     for (int r = 0; r < 8; ++r) each(r, p.wave % 4 * 16 + p.lane / 16 * 4 + r % 4, p.wave / 4 * 32 + r / 4 * 16 + p.lane % 16);
 }
 
+// The jobs of a launch: `kinds` for each of `cells` chunks.  A chunk's jobs follow one another on one of the eight dies (workgroups
+// go round the dies), so that what they share is in its L2.
+struct Jobs {
+    unsigned cells, kinds, n;
+    __device__ __forceinline__ Jobs(unsigned cells_, unsigned kinds_) : cells(cells_), kinds(kinds_), n(blockIdx.x / 8) {}
+    __device__ __forceinline__ unsigned cell() const { return n / kinds * 8 + blockIdx.x % 8; }
+    __device__ __forceinline__ unsigned kind() const { return n % kinds; }
+    __device__ __forceinline__ void next() { n += gridDim.x / 8; }
+};
+
 struct NoPower { __device__ uint32_t operator()(int, int) const { return 1; } };
 
 // P and W of a chunk, or one tile of its U.
 __global__ __launch_bounds__(kThreads) void k_chunk_open(ChunkArgs q)
 {
     extern __shared__ __attribute__((aligned(16))) u8 lds[];          // kOperands kOperand
-    const Place p = place();
-    const bool left = p.wave < 4;
+    const Place at_start = place();
+    const bool left = at_start.wave < 4;
     const Box box(q.box);
     const auto to_box = [&](int, const Quad& e1, const Quad& e0) { box.put(e1, e0); };
-    const unsigned kinds = 1 + q.mt * q.nt, jobs = (unsigned)q.B * q.H * q.chunks * kinds;
-    for (unsigned job = blockIdx.x; job < jobs; job += gridDim.x) {
-        const int kind = job % kinds, chunk = job / kinds % q.chunks;
-        const long long bh = job / kinds / q.chunks;
-        const int b = (int)bh / q.H, h = (int)bh % q.H, t0 = chunk * kChunk, L = q.T - t0 < kChunk ? q.T - t0 : kChunk;
+    for (Jobs job(q.cells, 1 + q.mt * q.nt); job.cell() < q.cells; job.next()) {
+        const Place p = anew(at_start);
+        const int kind = job.kind(), bh = job.cell() / q.chunks, chunk = job.cell() - bh * q.chunks;
+        const int b = bh / q.H, h = bh - b * q.H, t0 = chunk * kChunk, L = min(q.T - t0, kChunk);
         const int32_t* const pow = q.decay + h * (kChunk + 1);
-        const long long at = bh * q.T + t0;                       // the chunk's first token in the dense arrays
+        const long long at = (long long)bh * q.T + t0;            // the chunk's first token in the dense arrays
         const long long ok = b * q.k.b + h * q.k.h + t0 * q.k.t;
-        u64 z0[8] = {}, z1[8] = {};
+        u64 z0[8], z1[8];                                       // start from the addends: asked for first
         if (kind == 0) {
+            each_word(p, [&](int r, int i, int j) {
+                const unsigned o = min(i, L - 1) * kChunk + min(j, i);
+                z0[r] = (q.c_p[0] + at * kChunk)[o]; z1[r] = (q.c_p[1] + at * kChunk)[o];
+            });
             const long long oq = b * q.q.b + h * q.q.h + t0 * q.q.t;
             for (int k0 = 0; k0 < q.dk; k0 += 64) {
-                const Tile<true> t(p, L, q.dk - k0);
+                const Place ps = anew(p);
+                const Tile<true> t(ps, L, q.dk - k0);
                 const long long oa = at * q.dk + k0;
                 if (left) bring_masked<true, true, false>(lds, t, q.q.p[0] + oq + k0, q.q.p[1] + oq + k0, q.q.t, q.a_q[0] + oa, q.a_q[1] + oa, q.dk, NoPower{}, 0, to_box);
                 else bring_masked<false, true, false>(lds, t, q.k.p[0] + ok + k0, q.k.p[1] + ok + k0, q.k.t, q.a_k[0] + oa, q.a_k[1] + oa, q.dk, NoPower{}, 0, to_box);
-                multiply_all(lds, p, t, [&](int i) { Quad m = t.load(q.a_q[1] + oa, q.dk, i); t.clear(i, m); return m; }, z0, z1);
+                multiply_all(lds, ps, t, [&](int i) { Quad m = t.load(q.a_q[1] + oa, q.dk, i); t.clear(i, m); return m; }, z0, z1);
             }
-            u64 c0[8], c1[8], a0[8], a1[8], f[8];                  // all asked for together
-            each_word(p, [&](int r, int i, int j) {
-                const bool in = i < L && j <= i;
-                const long long o = in ? (at + i) * kChunk + j : at * kChunk;
-                c0[r] = q.c_p[0][o]; c1[r] = q.c_p[1][o]; a0[r] = q.a_w[0][o]; a1[r] = q.a_w[1][o]; f[r] = (uint32_t)pow[in ? i - j : 0];
+            const Place pe = anew(p);
+            u64 a0[8], a1[8]; uint32_t f[8];                     // all asked for together
+            each_word(pe, [&](int r, int i, int j) {
+                const unsigned o = min(i, L - 1) * kChunk + min(j, i);
+                a0[r] = (q.a_w[0] + at * kChunk)[o]; a1[r] = (q.a_w[1] + at * kChunk)[o]; f[r] = pow[max(i - j, 0)];
             });
-            each_word(p, [&](int r, int i, int j) {
-                if (i >= L || j > i) return;
-                const long long o = (at + i) * kChunk + j;
-                const u64 w0 = rescaled<0>(rescaled<0>(c0[r] + z0[r], q.bits) * f[r], q.bits);
-                const u64 w1 = rescaled<1>(rescaled<1>(c1[r] + z1[r], q.bits) * f[r], q.bits);
+            each_word(pe, [&](int r, int i, int j) {
+                const u64 w0 = rescaled<0>(rescaled<0>(z0[r], q.bits) * f[r], q.bits), w1 = rescaled<1>(rescaled<1>(z1[r], q.bits) * f[r], q.bits);
                 const u64 e0 = w0 - a0[r], e1 = w1 - a1[r];
+                if (i >= L || j > i) return;
+                const unsigned o = i * kChunk + j;
                 box.put(r, e1, e0);
-                q.w_x0[o] = w0 + e1; q.w_open[o] = e0 + e1;
+                (q.w_x0 + at * kChunk)[o] = w0 + e1; (q.w_open + at * kChunk)[o] = e0 + e1;
             });
         } else {
             const int m0 = (kind - 1) / q.nt * 64, n0 = (kind - 1) % q.nt * 64;      // contraction over the chunk's tokens
-            const Tile<false> tk(p, q.dk - m0, L), tv(p, q.dv - n0, L);
-            const long long oa = at * q.dk + m0, ov = b * q.v.b + h * q.v.h + t0 * q.v.t + n0, oav = at * q.dv + n0;
-            if (left) bring_masked<true, false, true>(lds, tk, q.k.p[0] + ok + m0, q.k.p[1] + ok + m0, q.k.t, q.a_kd[0] + oa, q.a_kd[1] + oa, q.dk,
-                    [&](int, int j) { const int k = tk.k(j); return (uint32_t)pow[k < L ? L - 1 - k : 0]; }, q.bits,
-                    [&](int, const Quad& e1, const Quad& e0) { if (n0 == 0) box.put(e1, e0); });
-            else bring_masked<false, false, false>(lds, tv, q.v.p[0] + ov, q.v.p[1] + ov, q.v.t, q.a_v[0] + oav, q.a_v[1] + oav, q.dv, NoPower{}, 0,
-                    [&](int i, const Quad& e1, const Quad& e0) {
-                        if (m0) return;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            if (!tv.has(i, j)) continue;
-                            const long long to = oav + tv.row(i) + tv.k(j) * q.dv;
-                            q.recv_v[0][to] = e1.w[j]; q.recv_v[1][to] = e0.w[j];
-                        }
-                    });
-            multiply_all(lds, p, tk, [&](int i) { Quad m = tk.load(q.a_kd[1] + oa, q.dk, i); tk.clear(i, m); return m; }, z0, z1);
-            const long long cell = (bh * q.chunks + chunk) * q.dk * q.dv;
-            u64 c0[8], c1[8];
-            each_word(p, [&](int r, int i, int jj) {
-                const int d = m0 + i, e = n0 + jj;
-                const long long o = cell + (d < q.dk && e < q.dv ? d * q.dv + e : 0);
-                c0[r] = q.c_u[0][o]; c1[r] = q.c_u[1][o];
+            const long long cell = (long long)job.cell() * q.dk * q.dv;
+            each_word(p, [&](int r, int i, int j) {
+                const unsigned o = min(m0 + i, q.dk - 1) * q.dv + min(n0 + j, q.dv - 1);
+                z0[r] = (q.c_u[0] + cell)[o]; z1[r] = (q.c_u[1] + cell)[o];
             });
-            each_word(p, [&](int r, int i, int jj) {
-                const int d = m0 + i, e = n0 + jj;
+            for (int j0 = 0; j0 < L; j0 += 64) {
+                const Place ps = anew(p);
+                const Tile<false> tk(ps, q.dk - m0, L - j0), tv(ps, q.dv - n0, L - j0);
+                const long long o = ok + j0 * q.k.t + m0, oa = (at + j0) * q.dk + m0;
+                const long long ov = b * q.v.b + h * q.v.h + (t0 + j0) * q.v.t + n0, oav = (at + j0) * q.dv + n0;
+                if (left) bring_masked<true, false, true>(lds, tk, q.k.p[0] + o, q.k.p[1] + o, q.k.t, q.a_kd[0] + oa, q.a_kd[1] + oa, q.dk,
+                        [&](int, int j) { return pow[max(L - 1 - j0 - tk.k(j), 0)]; }, q.bits,
+                        [&](int, const Quad& e1, const Quad& e0) { if (n0 == 0) box.put(e1, e0); });
+                else bring_masked<false, false, false>(lds, tv, q.v.p[0] + ov, q.v.p[1] + ov, q.v.t, q.a_v[0] + oav, q.a_v[1] + oav, q.dv, NoPower{}, 0,
+                        [&](int i, const Quad& e1, const Quad& e0) {
+                            if (m0) return;
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                if (!tv.has(i, j)) continue;
+                                const unsigned to = tv.row(i) + tv.k(j) * q.dv;
+                                (q.recv_v[0] + oav)[to] = e1.w[j]; (q.recv_v[1] + oav)[to] = e0.w[j];
+                            }
+                        });
+                multiply_all(lds, ps, tk, [&](int i) { Quad m = tk.load(q.a_kd[1] + oa, q.dk, i); tk.clear(i, m); return m; }, z0, z1);
+            }
+            each_word(anew(p), [&](int r, int i, int j) {
+                const int d = m0 + i, e = n0 + j;
                 if (d >= q.dk || e >= q.dv) return;
-                const long long o = cell + d * q.dv + e;
-                q.u[0][o] = c0[r] + z0[r]; q.u[1][o] = c1[r] + z1[r];
+                const unsigned o = d * q.dv + e;
+                (q.u[0] + cell)[o] = z0[r]; (q.u[1] + cell)[o] = z1[r];
             });
         }
     }
@@ -332,71 +357,72 @@ __global__ __launch_bounds__(256) void k_chunk_states(ChunkArgs q)
 __global__ __launch_bounds__(kThreads) void k_chunk_out(ChunkArgs q)
 {
     extern __shared__ __attribute__((aligned(16))) u8 lds[];          // kOperands kOperand
-    const Place p = place();
-    const bool left = p.wave < 4;
+    const Place at_start = place();
+    const bool left = at_start.wave < 4;
     const Box box(q.box);
-    const unsigned jobs = (unsigned)q.B * q.H * q.chunks * q.nt;
     struct Three { Quad own, open, mask; };
-    for (unsigned job = blockIdx.x; job < jobs; job += gridDim.x) {
-        const int n0 = (int)(job % q.nt) * 64, chunk = job / q.nt % q.chunks;
-        const long long bh = job / q.nt / q.chunks;
-        const int b = (int)bh / q.H, h = (int)bh % q.H, t0 = chunk * kChunk, L = q.T - t0 < kChunk ? q.T - t0 : kChunk;
+    for (Jobs job(q.cells, q.nt); job.cell() < q.cells; job.next()) {
+        const Place p = anew(at_start);
+        const int n0 = job.kind() * 64, bh = job.cell() / q.chunks, chunk = job.cell() - bh * q.chunks;
+        const int b = bh / q.H, h = bh - b * q.H, t0 = chunk * kChunk, L = min(q.T - t0, kChunk);
         const int32_t* const pow = q.decay + h * (kChunk + 1);
-        const long long at = bh * q.T + t0, ow = at * kChunk;
-        u64 z0[8] = {}, z1[8] = {};
-        const Tile<true> tw(p, L, kChunk);
-        const auto below = [&](int i, Quad& w) {                  // W: nothing above the diagonal
+        const long long at = (long long)bh * q.T + t0;
+        u64 z0[8], z1[8];
+        each_word(p, [&](int r, int i, int j) {
+            const unsigned o = min(i, L - 1) * q.dv + min(n0 + j, q.dv - 1);
+            z0[r] = (q.c_o[0] + at * q.dv)[o]; z1[r] = (q.c_o[1] + at * q.dv)[o];
+        });
+        for (int j0 = 0; j0 < L; j0 += 64) {
+            const Place ps = anew(p);
+            const Tile<true> tw(ps, L, 64);
+            const long long ow = at * kChunk + j0;
+            const auto below = [&](int i, Quad& w) {              // W: nothing above the diagonal
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const u64 keep = -(u64)(tw.row(i) < L && tw.k(j) <= tw.row(i));
-                w.w[j] &= keep;
+                for (int j = 0; j < 4; ++j) w.w[j] = tw.row(i) < L && j0 + tw.k(j) <= tw.row(i) ? w.w[j] : 0;
+            };
+            if (left) bring<true>(lds, tw, [&](int i) { return Three{ tw.load(q.w_x0 + ow, kChunk, i), tw.load(q.w_open + ow, kChunk, i), {} }; },
+                    [&](int i, const Three& r, Quad& own, Quad& open, Quad&) { own = r.own; open = r.open; below(i, own); below(i, open); });
+            else {
+                const long long o = b * q.v.b + h * q.v.h + (t0 + j0) * q.v.t + n0, oa = (at + j0) * q.dv + n0;
+                const Tile<false> t(ps, q.dv - n0, L - j0);
+                struct Raw { Quad v0, v1, a1, r0, r1; };
+                bring<false>(lds, t, [&](int i) { return Raw{ t.load(q.v.p[0] + o, q.v.t, i), t.load(q.v.p[1] + o, q.v.t, i), t.load(q.a_v[1] + oa, q.dv, i),
+                                                              t.load(q.recv_v[0] + oa, q.dv, i), t.load(q.recv_v[1] + oa, q.dv, i) }; },
+                    [&](int i, const Raw& r, Quad& own, Quad& open, Quad& mask) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) { own.w[j] = r.v0.w[j] + r.r0.w[j]; open.w[j] = r.v1.w[j] - r.a1.w[j] + r.r1.w[j]; }
+                        mask = r.a1;
+                        t.clear(i, own); t.clear(i, open); t.clear(i, mask);
+                    });
             }
-        };
-        if (left) bring<true>(lds, tw, [&](int i) { return Three{ tw.load(q.w_x0 + ow, kChunk, i), tw.load(q.w_open + ow, kChunk, i), {} }; },
-                [&](int i, const Three& r, Quad& own, Quad& open, Quad&) { own = r.own; open = r.open; below(i, own); below(i, open); });
-        else {
-            const long long o = b * q.v.b + h * q.v.h + t0 * q.v.t + n0, oa = at * q.dv + n0;
-            const Tile<false> t(p, q.dv - n0, L);
-            struct Raw { Quad v0, v1, a1, r0, r1; };
-            bring<false>(lds, t, [&](int i) { return Raw{ t.load(q.v.p[0] + o, q.v.t, i), t.load(q.v.p[1] + o, q.v.t, i), t.load(q.a_v[1] + oa, q.dv, i),
-                                                       t.load(q.recv_v[0] + oa, q.dv, i), t.load(q.recv_v[1] + oa, q.dv, i) }; },
-                [&](int i, const Raw& r, Quad& own, Quad& open, Quad& mask) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) { own.w[j] = r.v0.w[j] + r.r0.w[j]; open.w[j] = r.v1.w[j] - r.a1.w[j] + r.r1.w[j]; }
-                    mask = r.a1;
-                    t.clear(i, own); t.clear(i, open); t.clear(i, mask);
-                });
+            multiply_all(lds, ps, tw, [&](int i) { Quad m = tw.load(q.a_w[1] + ow, kChunk, i); below(i, m); return m; }, z0, z1);
         }
-        multiply_all(lds, p, tw, [&](int i) { Quad m = tw.load(q.a_w[1] + ow, kChunk, i); below(i, m); return m; }, z0, z1);
         for (int k0 = 0; k0 < q.dk; k0 += 64) {
-            const Tile<true> tq(p, L, q.dk - k0);
+            const Place ps = anew(p);
+            const Tile<true> tq(ps, L, q.dk - k0);
             const long long oa = at * q.dk + k0;
             if (left) {
                 const long long o = b * q.q.b + h * q.q.h + t0 * q.q.t + k0;
                 bring_masked<true, true, true>(lds, tq, q.q.p[0] + o, q.q.p[1] + o, q.q.t, q.a_qd[0] + oa, q.a_qd[1] + oa, q.dk,
-                    [&](int i, int) { const int row = tq.row(i); return (uint32_t)pow[row < L ? row + 1 : 0]; }, q.bits,
+                    [&](int i, int) { return pow[min(tq.row(i), L - 1) + 1]; }, q.bits,
                     [&](int, const Quad& e1, const Quad& e0) { if (n0 == 0) box.put(e1, e0); });
             } else {
-                const long long o = ((bh * q.chunks + chunk) * q.dk + k0) * q.dv + n0;
-                const Tile<false> t(p, q.dv - n0, q.dk - k0);
+                const long long o = ((long long)job.cell() * q.dk + k0) * q.dv + n0;
+                const Tile<false> t(ps, q.dv - n0, q.dk - k0);
                 bring<false>(lds, t, [&](int i) { return Three{ t.load(q.u[0] + o, q.dv, i), t.load(q.u[1] + o, q.dv, i), t.load(q.a_s[1] + o, q.dv, i) }; },
                     [&](int i, const Three& r, Quad& own, Quad& open, Quad& mask) {
                         own = r.own; open = r.open; mask = r.mask;
                         t.clear(i, own); t.clear(i, open); t.clear(i, mask);
                     });
             }
-            multiply_all(lds, p, tq, [&](int i) { Quad m = tq.load(q.a_qd[1] + oa, q.dk, i); tq.clear(i, m); return m; }, z0, z1);
+            multiply_all(lds, ps, tq, [&](int i) { Quad m = tq.load(q.a_qd[1] + oa, q.dk, i); tq.clear(i, m); return m; }, z0, z1);
         }
-        u64 c0[8], c1[8];
-        each_word(p, [&](int r, int i, int j) {
-            const long long o = at * q.dv + (i < L && n0 + j < q.dv ? i * q.dv + n0 + j : 0);
-            c0[r] = q.c_o[0][o]; c1[r] = q.c_o[1][o];
-        });
-        each_word(p, [&](int r, int i, int j) {
+        const long long to = b * q.ob + h * q.oh + t0 * q.ot + n0;
+        each_word(anew(p), [&](int r, int i, int j) {
             if (i >= L || n0 + j >= q.dv) return;
-            const long long o = b * q.ob + h * q.oh + (t0 + i) * q.ot + n0 + j;
-            q.o[0][o] = rescaled<0>(c0[r] + z0[r], q.bits);
-            q.o[1][o] = rescaled<1>(c1[r] + z1[r], q.bits);
+            const long long o = i * q.ot;
+            (q.o[0] + to)[o + j] = rescaled<0>(z0[r], q.bits);
+            (q.o[1] + to)[o + j] = rescaled<1>(z1[r], q.bits);
         });
     }
 }
@@ -578,13 +604,13 @@ int mpc_linear_attention(mpc_ctx* c, mpc_cshare q, mpc_cshare k, mpc_cshare v, m
     a.w_x0 = ws.take<u64>(p.w); a.w_open = ws.take<u64>(p.w); a.box = ws.take<u64>(p.box);
     if (!ws.ok) return MPC_ENOMEM;
     a.B = B; a.H = H; a.T = T; a.dk = dk; a.dv = dv; a.chunks = (int)p.chunks; a.bits = c->frac_bits;
-    a.mt = (dk + 63) / 64; a.nt = (dv + 63) / 64;
+    a.mt = (dk + 63) / 64; a.nt = (dv + 63) / 64; a.cells = (unsigned)((long long)B * H * p.chunks);
     const auto grid = [](long long jobs, long long most) { return dim3((unsigned)(jobs < most ? jobs : most)); };
-    const long long cells = (long long)B * H * p.chunks;
+    const long long rounds = (a.cells + 7) / 8 * 8;               // the same for every die
     MPC_TRY(lane_first(c));
-    k_chunk_open<<<grid(cells * (1 + a.mt * a.nt), kBoxes), kThreads, kOperands * kOperand, c->s[0]>>>(a);
+    k_chunk_open<<<grid(rounds * (1 + a.mt * a.nt), kBoxes), kThreads, kOperands * kOperand, c->s[0]>>>(a);
     k_chunk_states<<<grid(((long long)n_s / 8 + 255) / 256, kStateBoxes), 256, 0, c->s[0]>>>(a);
-    k_chunk_out<<<grid(cells * a.nt, kBoxes), kThreads, kOperands * kOperand, c->s[0]>>>(a);
+    k_chunk_out<<<grid(rounds * a.nt, kBoxes), kThreads, kOperands * kOperand, c->s[0]>>>(a);
     MPC_HIP(c, hipGetLastError());
     return lane_fanout(c);
 }
