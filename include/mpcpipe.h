@@ -565,7 +565,7 @@ int mpc_matvec4(mpc_ctx* ctx, mpc_cshare x, const uint8_t* w, const int32_t* sca
  * Material, masks a_* and addends c_*, uniform words like every triple; BH = B * H.  Party 0's addend has its local product
  * taken off (as mpc_matmul_fold does): c_0 + c_1 = products below - (party 0's own products).
  *   prompt: a_q, a_k, a_qd, a_kd [BH][T][dk] (masks of Q, K, Qd, Kd); a_v [BH][T][dv]; a_w [BH][T][64] (row of a token,
- *     column of the chunk's token; above the diagonal nothing is read, and a_w counts as zero in c_o);
+ *     column of the chunk's token; above the diagonal no word is used, and a_w counts as zero in c_o);
  *     a_s [BH][chunks][dk][dv] (mask of the state before each chunk);
  *     c_p [BH][T][64] of a_q a_k^T, c_u [BH][chunks][dk][dv] of a_kd^T a_v, c_o [BH][T][dv] of a_w a_v + a_qd a_s
  *   step: a_q, a_k [BH][dk], a_v [BH][dv], a_s [BH][dk][dv] (mask of S'); c_u [BH][dk][dv] of a_k a_v^T, c_o [BH][dv] of a_q a_s

@@ -7,8 +7,8 @@
 //   P = trunc(Q K^T), W[i][j] = trunc(P[i][j] pow[i-j]) for j <= i, else zero    Qd[i] = trunc(Q[i] pow[i+1])
 //   Kd[j] = trunc(K[j] pow[L-1-j]), U = Kd^T V                                   S' = trunc(pow[L] S + U)
 //   O = trunc([W | Qd] [V ; S])
-// Three launches: everything that one chunk has for itself (P, W, U and their openings), the states from chunk to chunk
-// (element by element), and O of all chunks.
+// Three launches: everything that one chunk has for itself (P, W and W V, U, and their openings), the states from chunk to chunk
+// (element by element), and the states' part of O.
 //
 // All products are Alg. 1 with party 0's local product folded into its addend (the folded calls of the linear layers):
 // party 0 has c_0 + (x_0 + e_1)(y_0 + f_1), party 1 has c_1 + e b_1 + a_1 f.  The exchange is by remote store: a masked word is
@@ -33,8 +33,7 @@ struct ChunkArgs {
     u64 *o[2]; long long ob, ot, oh;
     u64* state_out[2];
     const int32_t* decay;                     // [H][65]
-    u64* recv_v[2];                           // what the peer sent of V: [BH][T][dv]
-    u64 *w_x0, *w_open;                       // W: party 0's operand, opened words: [BH][T][64]
+    u64* part[2];                             // c_o + W V, not yet rescaled: [BH][T][dv]
     u64* u[2];                                // U; then the states: party 0's operand (u[0]) and opened words (u[1]): [BH][chunks][dk][dv]
     u64* box;
     int B, H, T, dk, dv, chunks, bits;
@@ -49,9 +48,10 @@ constexpr int kPlane = 64 * 64, kOperand = 8 * kPlane;      // bytes
 enum { kOwnLeft, kOwnRight, kOpenLeft, kMaskRight, kOpenRight, kOperands, kMaskLeft = kOwnLeft };
 
 // The first four waves bring the left operand, the others the right one: 16 words a thread, as four quads of rows 16 apart.
-// Wave w of the four has words 16w..16w+15 of the contraction; quad kq of them is {2kq, 2kq+1, 8+2kq, 9+2kq}, in the same order
-// for both operands, since a product does not care which.  Where a row's words are adjacent in memory (ADJACENT), four lanes read
-// 64 bytes of a row at once; else sixteen lanes read 128 bytes across the rows.  Stores to LDS meet every bank once either way.
+// Wave w of the four has words 16w..16w+15 of the contraction.  Where a row's words are adjacent in memory (ADJACENT), four lanes
+// read 64 bytes of a row at once, and quad kq is words {2kq, 2kq+1, 8+2kq, 9+2kq} (PAIRS): a product does not care about the order
+// if both operands have the same.  Elsewhere sixteen lanes read 128 bytes across the rows.  Stores to LDS meet every bank once
+// either way.
 struct Place { int wave, lane; };             // wave: the same for all lanes, read once (a scalar)
 __device__ __forceinline__ Place place() { return Place{ __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64)), (int)threadIdx.x % 64 }; }
 // The same place again: offsets and conditions that follow from the lane are made anew, instead of being kept (and spilled) across
@@ -60,15 +60,24 @@ __device__ __forceinline__ Place anew(Place p) { asm volatile("" : "+v"(p.lane))
 
 struct Quad { u64 w[4]; };
 
+// a quad's digits, from the place of its first one
+__device__ __forceinline__ void stage_at(u8* at, const Quad& q)
+{
+    uint32_t d[8];
+    digits_of_4(q.w, d);
+#pragma unroll
+    for (int p = 0; p < 8; ++p) *reinterpret_cast<uint32_t*>(at + p * kPlane) = d[p];
+}
+
 // A tile of `rows` rows and `cols` words along the contraction, at most 64 each of what is there; word (row, k) lies at
 // p + row*rs + k*ks words, one of the strides being 1 (ADJACENT: ks).  Rows and columns that are not there repeat the last one.
 // Offsets within a tile are below 2^31 bytes (kMaxStride).
-template <bool ADJACENT> struct Tile {
+template <bool ADJACENT, bool PAIRS = true> struct Tile {
     int rows, cols, row0, k0, quad;
     __device__ __forceinline__ Tile(const Place& p, int rows_, int cols_)
-        : rows(rows_), cols(cols_), row0(ADJACENT ? p.lane / 4 : p.lane % 16), quad(ADJACENT ? p.lane % 4 : p.lane / 16) { k0 = p.wave % 4 * 16 + quad * 2; }
+        : rows(rows_), cols(cols_), row0(ADJACENT ? p.lane / 4 : p.lane % 16), quad(ADJACENT ? p.lane % 4 : p.lane / 16) { k0 = p.wave % 4 * 16 + quad * (PAIRS ? 2 : 4); }
     __device__ __forceinline__ int row(int i) const { return row0 + i * 16; }
-    __device__ __forceinline__ int k(int j) const { return k0 + j % 2 + j / 2 * 8; }
+    __device__ __forceinline__ int k(int j) const { return PAIRS ? k0 + j % 2 + j / 2 * 8 : k0 + j; }
     __device__ __forceinline__ Quad load(const u64* p, long long stride, int i) const
     {
         const u8* const base = reinterpret_cast<const u8*>(p);
@@ -96,18 +105,14 @@ template <bool ADJACENT> struct Tile {
     }
     __device__ __forceinline__ void stage(u8* lds, int operand, int i, const Quad& q) const
     {
-        uint32_t d[8];
-        digits_of_4(q.w, d);
-        u8* const at = lds + operand * kOperand + k0 / 16 * 1024 + (row(i) * 16 + quad * 4);
-#pragma unroll
-        for (int p = 0; p < 8; ++p) *reinterpret_cast<uint32_t*>(at + p * kPlane) = d[p];
+        stage_at(lds + operand * kOperand + k0 / 16 * 1024 + (row(i) * 16 + quad * 4), q);
     }
 };
 
 // A thread's quads of an operand: load(i) asks for words, form(i, words, own0, open, mask1) makes party 0's operand x_0 + e_1, the
 // opened words and party 1's mask of them.  All words are asked for at once, ahead of the barrier behind which the last products'
 // operands may be written over: one after the other their latency was most of a job's time.
-template <bool LEFT, bool ADJACENT, class Load, class Form> __device__ __forceinline__ void bring(u8* lds, const Tile<ADJACENT>& t, Load load, Form form)
+template <bool LEFT, class T, class Load, class Form> __device__ __forceinline__ void bring(u8* lds, const T& t, Load load, Form form)
 {
     const decltype(load(0)) words[4] = { load(0), load(1), load(2), load(3) };
     __syncthreads();
@@ -121,30 +126,35 @@ template <bool LEFT, bool ADJACENT, class Load, class Form> __device__ __forcein
     }
 }
 
-// A masked operand: words of a sharing and of its mask; a word's power(i, j) is a public factor, followed by the rescale (DECAY);
-// sent(i, j, to party 0, to party 1).
-template <bool LEFT, bool ADJACENT, bool DECAY, class Power, class Sent>
-__device__ __forceinline__ void bring_masked(u8* lds, const Tile<ADJACENT>& t, const u64* x0, const u64* x1, long long stride,
+// Words of a sharing and of its mask, with the public factor of each word.
+struct Masked { Quad x0, x1, a0, a1; uint32_t f[4]; };
+template <bool DECAY> __device__ __forceinline__ void open_quad(const Masked& r, int bits, Quad& own, Quad& open, Quad& e0, Quad& e1)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        u64 w0 = r.x0.w[j], w1 = r.x1.w[j];
+        if (DECAY) { w0 = rescaled<0>(w0 * r.f[j], bits); w1 = rescaled<1>(w1 * r.f[j], bits); }
+        e0.w[j] = w0 - r.a0.w[j]; e1.w[j] = w1 - r.a1.w[j];
+        own.w[j] = w0 + e1.w[j]; open.w[j] = e0.w[j] + e1.w[j];
+    }
+}
+// A masked operand: a word's power(i, j) is a public factor, followed by the rescale (DECAY); sent(to party 0, to party 1).
+template <bool LEFT, bool DECAY, class T, class Power, class Sent>
+__device__ __forceinline__ void bring_masked(u8* lds, const T& t, const u64* x0, const u64* x1, long long stride,
                                              const u64* a0, const u64* a1, long long a_stride, Power power, int bits, Sent sent)
 {
-    struct Raw { Quad x0, x1, a0, a1; uint32_t f[4]; };
     bring<LEFT>(lds, t, [&](int i) {
-            Raw r{ t.load(x0, stride, i), t.load(x1, stride, i), t.load(a0, a_stride, i), t.load(a1, a_stride, i), {} };
+            Masked r{ t.load(x0, stride, i), t.load(x1, stride, i), t.load(a0, a_stride, i), t.load(a1, a_stride, i), {} };
             if (DECAY)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) r.f[j] = power(i, j);
             return r;
         },
-        [&](int i, const Raw& r, Quad& own, Quad& open, Quad& mask) {
+        [&](int i, const Masked& r, Quad& own, Quad& open, Quad& mask) {
             Quad e0, e1;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                u64 w0 = r.x0.w[j], w1 = r.x1.w[j];
-                if (DECAY) { w0 = rescaled<0>(w0 * r.f[j], bits); w1 = rescaled<1>(w1 * r.f[j], bits); }
-                e0.w[j] = w0 - r.a0.w[j]; e1.w[j] = w1 - r.a1.w[j];
-                own.w[j] = w0 + e1.w[j]; open.w[j] = e0.w[j] + e1.w[j]; mask.w[j] = r.a1.w[j];
-            }
-            sent(i, e1, e0);
+            open_quad<DECAY>(r, bits, own, open, e0, e1);
+            mask = r.a1;
+            sent(e1, e0);
             t.clear(i, own); t.clear(i, open); t.clear(i, mask);
         });
 }
@@ -162,7 +172,6 @@ struct Box {
             *reinterpret_cast<u64x2u*>(to1 + j * kThreads) = u64x2u{ e0.w[j], e0.w[j + 1] };
         }
     }
-    __device__ __forceinline__ void put(int r, u64 e1, u64 e0) const { to0[r % 2 + r / 2 % 2 * 2 * kThreads] = e1; to1[r % 2 + r / 2 % 2 * 2 * kThreads] = e0; }
 };
 
 // A wave has 16 rows and two tiles of 16 columns; acc[tile][s] sums the products of digits i + j = s.  One K step of 64 adds at
@@ -211,25 +220,34 @@ __device__ __forceinline__ void join(const Sums& a, u64 (&z)[8])
         }
 }
 
-// z0 += own0 own0', z1 += open mask1' + mask1 open' once both operands are in LDS.  Party 1's mask of the left operand, mask(i),
-// is asked for under the first two products and takes the place of party 0's operand: all waves bring it, two quads each.
-template <bool ADJACENT, class Mask> __device__ __forceinline__ void multiply_all(u8* lds, const Place& p, const Tile<ADJACENT>& t, Mask mask, u64 (&z0)[8], u64 (&z1)[8])
+// z0 += own0 own0', z1 += open mask1' + mask1 open' once both operands are in LDS.  ask() is for what third() needs, which puts
+// party 1's mask of the left operand in the place of party 0's operand, under the first two products.
+template <class Ask, class Third> __device__ __forceinline__ void multiply_all(u8* lds, const Place& p, Ask ask, Third third, u64 (&z0)[8], u64 (&z1)[8])
 {
-    const int first = p.wave / 4 * 2;
     Sums a;
     clear(a);
-    const Quad m0 = mask(first), m1 = mask(first + 1);
+    ask();
     __syncthreads();
     multiply(lds, p, kOwnLeft, kOwnRight, a);
     join(a, z0);
     clear(a);
     multiply(lds, p, kOpenLeft, kMaskRight, a);
     __syncthreads();
-    t.stage(lds, kMaskLeft, first, m0);
-    t.stage(lds, kMaskLeft, first + 1, m1);
+    third();
     __syncthreads();
     multiply(lds, p, kMaskLeft, kOpenRight, a);
     join(a, z1);
+}
+// the same with the mask of a left operand that lies in memory: all waves bring it, two quads each
+template <class T> __device__ __forceinline__ void multiply_all(u8* lds, const Place& p, const T& t, const u64* a1, long long stride, u64 (&z0)[8], u64 (&z1)[8])
+{
+    const int first = p.wave / 4 * 2;
+    Quad m[2];
+    multiply_all(lds, p, [&] { m[0] = t.load(a1, stride, first); m[1] = t.load(a1, stride, first + 1); },
+        [&] {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) { t.clear(first + i, m[i]); t.stage(lds, kMaskLeft, first + i, m[i]); }
+        }, z0, z1);
 }
 // each(index, row, column) of a thread's words of the product
 template <class Each> __device__ __forceinline__ void each_word(const Place& p, Each each)
@@ -239,61 +257,105 @@ template <class Each> __device__ __forceinline__ void each_word(const Place& p, 
 }
 
 // The jobs of a launch: `kinds` for each of `cells` chunks.  A chunk's jobs follow one another on one of the eight dies (workgroups
-// go round the dies), so that what they share is in its L2.
+// go round the dies), so that what they share is in its L2.  Where a workgroup would come to the same kind every time, the kinds
+// take turns from round to round: they differ in length (8 x 512 tokens of 12 heads, this launch 269 -> 218 us).
 struct Jobs {
-    unsigned cells, kinds, n;
-    __device__ __forceinline__ Jobs(unsigned cells_, unsigned kinds_) : cells(cells_), kinds(kinds_), n(blockIdx.x / 8) {}
+    unsigned cells, kinds, step, n;
+    bool turns;
+    __device__ __forceinline__ Jobs(unsigned cells_, unsigned kinds_) : cells(cells_), kinds(kinds_), step(gridDim.x / 8), n(blockIdx.x / 8) { turns = step % kinds == 0; }
     __device__ __forceinline__ unsigned cell() const { return n / kinds * 8 + blockIdx.x % 8; }
-    __device__ __forceinline__ unsigned kind() const { return n % kinds; }
-    __device__ __forceinline__ void next() { n += gridDim.x / 8; }
+    __device__ __forceinline__ unsigned kind() const { return (n + (turns ? n / step : 0)) % kinds; }
+    __device__ __forceinline__ void next() { n += step; }
 };
 
 struct NoPower { __device__ uint32_t operator()(int, int) const { return 1; } };
 
-// P and W of a chunk, or one tile of its U.
+// P, W and W V of a chunk, or one tile of its U.
 __global__ __launch_bounds__(kThreads) void k_chunk_open(ChunkArgs q)
 {
     extern __shared__ __attribute__((aligned(16))) u8 lds[];          // kOperands kOperand
     const Place at_start = place();
     const bool left = at_start.wave < 4;
     const Box box(q.box);
-    const auto to_box = [&](int, const Quad& e1, const Quad& e0) { box.put(e1, e0); };
+    const auto to_box = [&](const Quad& e1, const Quad& e0) { box.put(e1, e0); };
     for (Jobs job(q.cells, 1 + q.mt * q.nt); job.cell() < q.cells; job.next()) {
         const Place p = anew(at_start);
         const int kind = job.kind(), bh = job.cell() / q.chunks, chunk = job.cell() - bh * q.chunks;
         const int b = bh / q.H, h = bh - b * q.H, t0 = chunk * kChunk, L = min(q.T - t0, kChunk);
         const int32_t* const pow = q.decay + h * (kChunk + 1);
         const long long at = (long long)bh * q.T + t0;            // the chunk's first token in the dense arrays
-        const long long ok = b * q.k.b + h * q.k.h + t0 * q.k.t;
-        u64 z0[8], z1[8];                                       // start from the addends: asked for first
+        const long long ok = b * q.k.b + h * q.k.h + t0 * q.k.t, ov = b * q.v.b + h * q.v.h + t0 * q.v.t;
+        u64 z0[8], z1[8];                                         // start from the addends, asked for first
         if (kind == 0) {
-            each_word(p, [&](int r, int i, int j) {
-                const unsigned o = min(i, L - 1) * kChunk + min(j, i);
-                z0[r] = (q.c_p[0] + at * kChunk)[o]; z1[r] = (q.c_p[1] + at * kChunk)[o];
-            });
+            // P turned round, K Q^T: a thread's four words of a column are neighbours in a row of W, a quad of the next product
+            const int turned = p.wave % 4 * 16 + p.lane / 16 * 4, i0 = p.wave / 4 * 32 + p.lane % 16;    // j of its first word, i of tile 0
+            const auto quad_at = [&](const u64* w, int t) {       // of [token][64]
+                const u64* const from = w + at * kChunk + (unsigned)(min(i0 + t * 16, L - 1) * kChunk + turned);
+                const u64x2u lo = *reinterpret_cast<const u64x2u*>(from), hi = *reinterpret_cast<const u64x2u*>(from + 2);
+                return Quad{ { lo.x, lo.y, hi.x, hi.y } };
+            };
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const Quad c0 = quad_at(q.c_p[0], t), c1 = quad_at(q.c_p[1], t);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) { z0[t * 4 + j] = c0.w[j]; z1[t * 4 + j] = c1.w[j]; }
+            }
             const long long oq = b * q.q.b + h * q.q.h + t0 * q.q.t;
             for (int k0 = 0; k0 < q.dk; k0 += 64) {
                 const Place ps = anew(p);
                 const Tile<true> t(ps, L, q.dk - k0);
                 const long long oa = at * q.dk + k0;
-                if (left) bring_masked<true, true, false>(lds, t, q.q.p[0] + oq + k0, q.q.p[1] + oq + k0, q.q.t, q.a_q[0] + oa, q.a_q[1] + oa, q.dk, NoPower{}, 0, to_box);
-                else bring_masked<false, true, false>(lds, t, q.k.p[0] + ok + k0, q.k.p[1] + ok + k0, q.k.t, q.a_k[0] + oa, q.a_k[1] + oa, q.dk, NoPower{}, 0, to_box);
-                multiply_all(lds, ps, t, [&](int i) { Quad m = t.load(q.a_q[1] + oa, q.dk, i); t.clear(i, m); return m; }, z0, z1);
+                if (left) bring_masked<true, false>(lds, t, q.k.p[0] + ok + k0, q.k.p[1] + ok + k0, q.k.t, q.a_k[0] + oa, q.a_k[1] + oa, q.dk, NoPower{}, 0, to_box);
+                else bring_masked<false, false>(lds, t, q.q.p[0] + oq + k0, q.q.p[1] + oq + k0, q.q.t, q.a_q[0] + oa, q.a_q[1] + oa, q.dk, NoPower{}, 0, to_box);
+                multiply_all(lds, ps, t, q.a_k[1] + oa, q.dk, z0, z1);
             }
-            const Place pe = anew(p);
-            u64 a0[8], a1[8]; uint32_t f[8];                     // all asked for together
-            each_word(pe, [&](int r, int i, int j) {
-                const unsigned o = min(i, L - 1) * kChunk + min(j, i);
-                a0[r] = (q.a_w[0] + at * kChunk)[o]; a1[r] = (q.a_w[1] + at * kChunk)[o]; f[r] = pow[max(i - j, 0)];
-            });
-            each_word(pe, [&](int r, int i, int j) {
-                const u64 w0 = rescaled<0>(rescaled<0>(z0[r], q.bits) * f[r], q.bits), w1 = rescaled<1>(rescaled<1>(z1[r], q.bits) * f[r], q.bits);
-                const u64 e0 = w0 - a0[r], e1 = w1 - a1[r];
-                if (i >= L || j > i) return;
-                const unsigned o = i * kChunk + j;
-                box.put(r, e1, e0);
-                (q.w_x0 + at * kChunk)[o] = w0 + e1; (q.w_open + at * kChunk)[o] = e0 + e1;
-            });
+            Quad own[2], open[2], mask[2];                        // W
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const Quad a0 = quad_at(q.a_w[0], t), a1 = quad_at(q.a_w[1], t);
+                const int i = i0 + t * 16;
+                Quad e0, e1;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t f = pow[max(i - turned - j, 0)];
+                    const u64 w0 = rescaled<0>(rescaled<0>(z0[t * 4 + j], q.bits) * f, q.bits), w1 = rescaled<1>(rescaled<1>(z1[t * 4 + j], q.bits) * f, q.bits);
+                    const bool below = i < L && turned + j <= i;  // nothing above the diagonal
+                    e0.w[j] = below ? w0 - a0.w[j] : 0; e1.w[j] = below ? w1 - a1.w[j] : 0;
+                    own[t].w[j] = below ? w0 + e1.w[j] : 0; open[t].w[j] = e0.w[j] + e1.w[j]; mask[t].w[j] = below ? a1.w[j] : 0;
+                }
+                box.put(e1, e0);
+            }
+            for (int n0 = 0; n0 < q.dv; n0 += 64) {
+                const Place ps = anew(p);
+                const Tile<false, false> tv(ps, q.dv - n0, L);
+                const long long oa = at * q.dv + n0, o = ov + n0;
+                const int first = ps.wave / 4 * 2;                // all waves bring V, two quads each
+                Masked v[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    v[i] = Masked{ tv.load(q.v.p[0] + o, q.v.t, first + i), tv.load(q.v.p[1] + o, q.v.t, first + i),
+                                   tv.load(q.a_v[0] + oa, q.dv, first + i), tv.load(q.a_v[1] + oa, q.dv, first + i), {} };
+                each_word(ps, [&](int r, int i, int j) {
+                    const unsigned at_o = min(i, L - 1) * q.dv + min(j, q.dv - n0 - 1);
+                    z0[r] = (q.c_o[0] + oa)[at_o]; z1[r] = (q.c_o[1] + oa)[at_o];
+                });
+                u8* const w_at = lds + ps.wave % 4 * 1024 + ((ps.wave / 4 * 32 + ps.lane % 16) * 16 + ps.lane / 16 * 4);
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    Quad vo, vp, e0, e1;
+                    open_quad<false>(v[i], 0, vo, vp, e0, e1);    // sent with U's tiles
+                    tv.clear(first + i, vo); tv.clear(first + i, vp); tv.clear(first + i, v[i].a1);
+                    tv.stage(lds, kOwnRight, first + i, vo); tv.stage(lds, kOpenRight, first + i, vp); tv.stage(lds, kMaskRight, first + i, v[i].a1);
+                    stage_at(w_at + kOwnLeft * kOperand + i * 256, own[i]);
+                    stage_at(w_at + kOpenLeft * kOperand + i * 256, open[i]);
+                }
+                multiply_all(lds, ps, [] {}, [&] { stage_at(w_at + kMaskLeft * kOperand, mask[0]); stage_at(w_at + kMaskLeft * kOperand + 256, mask[1]); }, z0, z1);
+                each_word(anew(p), [&](int r, int i, int j) {
+                    if (i >= L || n0 + j >= q.dv) return;
+                    (q.part[0] + oa)[(unsigned)(i * q.dv + j)] = z0[r]; (q.part[1] + oa)[(unsigned)(i * q.dv + j)] = z1[r];
+                });
+            }
         } else {
             const int m0 = (kind - 1) / q.nt * 64, n0 = (kind - 1) % q.nt * 64;      // contraction over the chunk's tokens
             const long long cell = (long long)job.cell() * q.dk * q.dv;
@@ -301,26 +363,14 @@ __global__ __launch_bounds__(kThreads) void k_chunk_open(ChunkArgs q)
                 const unsigned o = min(m0 + i, q.dk - 1) * q.dv + min(n0 + j, q.dv - 1);
                 z0[r] = (q.c_u[0] + cell)[o]; z1[r] = (q.c_u[1] + cell)[o];
             });
-            for (int j0 = 0; j0 < L; j0 += 64) {
-                const Place ps = anew(p);
-                const Tile<false> tk(ps, q.dk - m0, L - j0), tv(ps, q.dv - n0, L - j0);
-                const long long o = ok + j0 * q.k.t + m0, oa = (at + j0) * q.dk + m0;
-                const long long ov = b * q.v.b + h * q.v.h + (t0 + j0) * q.v.t + n0, oav = (at + j0) * q.dv + n0;
-                if (left) bring_masked<true, false, true>(lds, tk, q.k.p[0] + o, q.k.p[1] + o, q.k.t, q.a_kd[0] + oa, q.a_kd[1] + oa, q.dk,
-                        [&](int, int j) { return pow[max(L - 1 - j0 - tk.k(j), 0)]; }, q.bits,
-                        [&](int, const Quad& e1, const Quad& e0) { if (n0 == 0) box.put(e1, e0); });
-                else bring_masked<false, false, false>(lds, tv, q.v.p[0] + ov, q.v.p[1] + ov, q.v.t, q.a_v[0] + oav, q.a_v[1] + oav, q.dv, NoPower{}, 0,
-                        [&](int i, const Quad& e1, const Quad& e0) {
-                            if (m0) return;
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                if (!tv.has(i, j)) continue;
-                                const unsigned to = tv.row(i) + tv.k(j) * q.dv;
-                                (q.recv_v[0] + oav)[to] = e1.w[j]; (q.recv_v[1] + oav)[to] = e0.w[j];
-                            }
-                        });
-                multiply_all(lds, ps, tk, [&](int i) { Quad m = tk.load(q.a_kd[1] + oa, q.dk, i); tk.clear(i, m); return m; }, z0, z1);
-            }
+            const Tile<false, false> tk(p, q.dk - m0, L), tv(p, q.dv - n0, L);
+            const long long oa = at * q.dk + m0, oav = at * q.dv + n0;
+            if (left) bring_masked<true, true>(lds, tk, q.k.p[0] + ok + m0, q.k.p[1] + ok + m0, q.k.t, q.a_kd[0] + oa, q.a_kd[1] + oa, q.dk,
+                    [&](int, int j) { return pow[max(L - 1 - tk.k(j), 0)]; }, q.bits,
+                    [&](const Quad& e1, const Quad& e0) { if (n0 == 0) box.put(e1, e0); });
+            else bring_masked<false, false>(lds, tv, q.v.p[0] + ov + n0, q.v.p[1] + ov + n0, q.v.t, q.a_v[0] + oav, q.a_v[1] + oav, q.dv, NoPower{}, 0,
+                    [&](const Quad& e1, const Quad& e0) { if (m0 == 0) box.put(e1, e0); });
+            multiply_all(lds, p, tk, q.a_kd[1] + oa, q.dk, z0, z1);
             each_word(anew(p), [&](int r, int i, int j) {
                 const int d = m0 + i, e = n0 + j;
                 if (d >= q.dk || e >= q.dv) return;
@@ -353,7 +403,7 @@ __global__ __launch_bounds__(256) void k_chunk_states(ChunkArgs q)
     }
 }
 
-// O of a chunk, 64 columns of dv: first the part within the chunk, then the state's.
+// O of a chunk, 64 columns of dv: the states' part joins what the chunk has for itself.
 __global__ __launch_bounds__(kThreads) void k_chunk_out(ChunkArgs q)
 {
     extern __shared__ __attribute__((aligned(16))) u8 lds[];          // kOperands kOperand
@@ -370,42 +420,17 @@ __global__ __launch_bounds__(kThreads) void k_chunk_out(ChunkArgs q)
         u64 z0[8], z1[8];
         each_word(p, [&](int r, int i, int j) {
             const unsigned o = min(i, L - 1) * q.dv + min(n0 + j, q.dv - 1);
-            z0[r] = (q.c_o[0] + at * q.dv)[o]; z1[r] = (q.c_o[1] + at * q.dv)[o];
+            z0[r] = (q.part[0] + at * q.dv)[o]; z1[r] = (q.part[1] + at * q.dv)[o];
         });
-        for (int j0 = 0; j0 < L; j0 += 64) {
-            const Place ps = anew(p);
-            const Tile<true> tw(ps, L, 64);
-            const long long ow = at * kChunk + j0;
-            const auto below = [&](int i, Quad& w) {              // W: nothing above the diagonal
-#pragma unroll
-                for (int j = 0; j < 4; ++j) w.w[j] = tw.row(i) < L && j0 + tw.k(j) <= tw.row(i) ? w.w[j] : 0;
-            };
-            if (left) bring<true>(lds, tw, [&](int i) { return Three{ tw.load(q.w_x0 + ow, kChunk, i), tw.load(q.w_open + ow, kChunk, i), {} }; },
-                    [&](int i, const Three& r, Quad& own, Quad& open, Quad&) { own = r.own; open = r.open; below(i, own); below(i, open); });
-            else {
-                const long long o = b * q.v.b + h * q.v.h + (t0 + j0) * q.v.t + n0, oa = (at + j0) * q.dv + n0;
-                const Tile<false> t(ps, q.dv - n0, L - j0);
-                struct Raw { Quad v0, v1, a1, r0, r1; };
-                bring<false>(lds, t, [&](int i) { return Raw{ t.load(q.v.p[0] + o, q.v.t, i), t.load(q.v.p[1] + o, q.v.t, i), t.load(q.a_v[1] + oa, q.dv, i),
-                                                              t.load(q.recv_v[0] + oa, q.dv, i), t.load(q.recv_v[1] + oa, q.dv, i) }; },
-                    [&](int i, const Raw& r, Quad& own, Quad& open, Quad& mask) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) { own.w[j] = r.v0.w[j] + r.r0.w[j]; open.w[j] = r.v1.w[j] - r.a1.w[j] + r.r1.w[j]; }
-                        mask = r.a1;
-                        t.clear(i, own); t.clear(i, open); t.clear(i, mask);
-                    });
-            }
-            multiply_all(lds, ps, tw, [&](int i) { Quad m = tw.load(q.a_w[1] + ow, kChunk, i); below(i, m); return m; }, z0, z1);
-        }
         for (int k0 = 0; k0 < q.dk; k0 += 64) {
             const Place ps = anew(p);
             const Tile<true> tq(ps, L, q.dk - k0);
             const long long oa = at * q.dk + k0;
             if (left) {
                 const long long o = b * q.q.b + h * q.q.h + t0 * q.q.t + k0;
-                bring_masked<true, true, true>(lds, tq, q.q.p[0] + o, q.q.p[1] + o, q.q.t, q.a_qd[0] + oa, q.a_qd[1] + oa, q.dk,
+                bring_masked<true, true>(lds, tq, q.q.p[0] + o, q.q.p[1] + o, q.q.t, q.a_qd[0] + oa, q.a_qd[1] + oa, q.dk,
                     [&](int i, int) { return pow[min(tq.row(i), L - 1) + 1]; }, q.bits,
-                    [&](int, const Quad& e1, const Quad& e0) { if (n0 == 0) box.put(e1, e0); });
+                    [&](const Quad& e1, const Quad& e0) { if (n0 == 0) box.put(e1, e0); });
             } else {
                 const long long o = ((long long)job.cell() * q.dk + k0) * q.dv + n0;
                 const Tile<false> t(ps, q.dv - n0, q.dk - k0);
@@ -415,7 +440,7 @@ __global__ __launch_bounds__(kThreads) void k_chunk_out(ChunkArgs q)
                         t.clear(i, own); t.clear(i, open); t.clear(i, mask);
                     });
             }
-            multiply_all(lds, ps, tq, [&](int i) { Quad m = tq.load(q.a_qd[1] + oa, q.dk, i); tq.clear(i, m); return m; }, z0, z1);
+            multiply_all(lds, ps, tq, q.a_qd[1] + oa, q.dk, z0, z1);
         }
         const long long to = b * q.ob + h * q.oh + t0 * q.ot + n0;
         each_word(anew(p), [&](int r, int i, int j) {
@@ -538,14 +563,14 @@ int shape_ok(mpc_ctx* c, int B, int T, int H, int dk, int dv)
     return c && c->frac_bits > 30 ? MPC_ERANGE : MPC_OK;       // a decay of one has to fit 31 bits
 }
 
-struct ChunkPlan { size_t recv, w, u, box, total; long long chunks; };
+struct ChunkPlan { size_t part, u, box, total; long long chunks; };
 ChunkPlan plan(int B, int T, int H, int dk, int dv)
 {
     ChunkPlan p{};
     const size_t BH = (size_t)B * H;
     p.chunks = (T + kChunk - 1) / kChunk;
-    p.recv = BH * T * dv; p.w = BH * T * kChunk; p.u = BH * p.chunks * dk * dv; p.box = kStateBoxes * 512 > kBoxes * 2 * kBoxWords ? kStateBoxes * 512 : kBoxes * 2 * kBoxWords;
-    p.total = 2 * align_up(p.recv * 8) + 2 * align_up(p.w * 8) + 2 * align_up(p.u * 8) + align_up(p.box * 8);
+    p.part = BH * T * dv; p.u = BH * p.chunks * dk * dv; p.box = kStateBoxes * 512 > kBoxes * 2 * kBoxWords ? kStateBoxes * 512 : kBoxes * 2 * kBoxWords;
+    p.total = 2 * align_up(p.part * 8) + 2 * align_up(p.u * 8) + align_up(p.box * 8);
     return p;
 }
 
@@ -599,9 +624,9 @@ int mpc_linear_attention(mpc_ctx* c, mpc_cshare q, mpc_cshare k, mpc_cshare v, m
         a.a_q[i] = m->a_q.p[i]; a.a_k[i] = m->a_k.p[i]; a.a_qd[i] = m->a_qd.p[i]; a.a_kd[i] = m->a_kd.p[i]; a.a_v[i] = m->a_v.p[i];
         a.a_w[i] = m->a_w.p[i]; a.a_s[i] = m->a_s.p[i]; a.c_p[i] = m->c_p.p[i]; a.c_u[i] = m->c_u.p[i]; a.c_o[i] = m->c_o.p[i];
         a.state[i] = state.p[i]; a.o[i] = o.p[i]; a.state_out[i] = state_out.p[i];
-        a.recv_v[i] = ws.take<u64>(p.recv); a.u[i] = ws.take<u64>(p.u);
+        a.part[i] = ws.take<u64>(p.part); a.u[i] = ws.take<u64>(p.u);
     }
-    a.w_x0 = ws.take<u64>(p.w); a.w_open = ws.take<u64>(p.w); a.box = ws.take<u64>(p.box);
+    a.box = ws.take<u64>(p.box);
     if (!ws.ok) return MPC_ENOMEM;
     a.B = B; a.H = H; a.T = T; a.dk = dk; a.dv = dv; a.chunks = (int)p.chunks; a.bits = c->frac_bits;
     a.mt = (dk + 63) / 64; a.nt = (dv + 63) / 64; a.cells = (unsigned)((long long)B * H * p.chunks);
