@@ -4,8 +4,9 @@
 //
 // On the matrix cores the weights are the left operand, 16 rows, and a row of x is the right one: its 16 columns are the eight
 // digits of both parties' words, so one 16 x 16 x 64 product serves a whole row.  The digit sums of a group are exact in 32
-// bits, times the group's scale they are added up in 64, and the eight digits join at the end.  Bound by reading the weights
-// (25088 x 4096: 51 MB) where there are many, by latency and the scales' 64-bit products where there are few.
+// bits, times the group's scale they are added up in 64, and the eight digits join at the end.  One row of 25088 x 4096 takes
+// 18 us (51 MB of weights, 2.9 TB/s): every workgroup also reads x, twice the bytes of its weights out of the L2, and without either
+// of the two it takes 12.  Several rows are bound by the digits' and the scales' vector instructions, few weights by latency.
 #include "attention.h"
 #include "digits.h"
 
@@ -17,11 +18,16 @@ typedef int i32x2 __attribute__((ext_vector_type(2)));
 struct MatvecArgs {
     const u64* x[2]; u64* z[2];
     const u8* w; const int32_t* scales;
-    int M, K, N, group, groups, row_bytes, shift;
+    uint32_t* digits;                     // digits in memory, or none
+    int M, K, N, group, groups, row_bytes, shift, blocks;
 };
 
 constexpr int kBlock = 256;                   // columns that a wave takes at a time
-constexpr int most_waves(int mt) { return mt <= 2 ? 16 : 8; }
+constexpr int most_waves(int mt) { return mt == 1 ? 16 : 8; }
+
+// Whether the digits of x are made once, by a launch of their own, instead of by every workgroup for itself.  us with and without:
+// 8 x 25088 x 4096 51 / 76, 16 x 4096 x 4096 33 / 44; but 4 x 4096 x 4096 12 / 12, 8 x 1024 x 4096 13 / 11, 1 x 768 x 2304 7 / 4.
+bool digits_in_memory(int M, int K, int N) { return M > 4 && (long long)M * K * N >= 1ll << 27; }
 
 // The digits of a block of x in LDS, as the lanes of a product read them: for every set of G columns (kg: a quarter of them) and
 // column c = 8 party + digit, the words' bytes in the order in which a lane's weights come out of their halves, even columns
@@ -41,22 +47,68 @@ template <int G> struct Digits {
     }
 };
 
-// A workgroup has 16 rows of the weights and MT rows of x; its waves share the columns, a block at a time.
-template <int G, int MT>
+// The same digits in memory, made once for all workgroups: what a lane needs of a block, 16 dwords, as four pieces of 16 bytes,
+// [row][block][piece][lane].
+template <int G> __global__ __launch_bounds__(256) void k_digits4(MatvecArgs q)
+{
+    const int g8 = threadIdx.x % 32, party = threadIdx.x / 32 % 2, block = blockIdx.x * 4 + threadIdx.x / 64, m = blockIdx.y;
+    if (block >= q.blocks) return;
+    u64 v[8];
+    const u64* const row = q.x[party] + (size_t)m * q.K;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) { const int k = block * kBlock + g8 * 8 + j; const u64 t = row[min(k, q.K - 1)]; v[j] = k < q.K ? t : 0; }
+    uint32_t* const to = q.digits + ((size_t)m * q.blocks + block) * 1024;
+#pragma unroll
+    for (int odd = 0; odd < 2; ++odd) {
+        const u64 four[4] = { v[odd], v[2 + odd], v[4 + odd], v[6 + odd] };
+        uint32_t d[8];
+        digits_of_4(four, d);
+        const int i = G == 128 ? g8 / 16 * 8 + odd * 4 + g8 % 4 : G == 64 ? g8 / 8 * 4 + odd * 2 + g8 % 2 : g8 / 4 * 2 + odd;
+        const int kg = G == 128 ? g8 % 16 / 4 : G == 64 ? g8 % 8 / 2 : g8 % 4;
+#pragma unroll
+        for (int p = 0; p < 8; ++p) to[i / 4 * 256 + (kg * 16 + party * 8 + p) * 4 + i % 4] = d[p];
+    }
+}
+
+// A workgroup has 16 rows of the weights and MT rows of x; its waves share the columns, a block at a time.  MADE: the digits are
+// in memory, else a wave makes those of its blocks.
+template <int G, int MT, bool MADE>
 __global__ __launch_bounds__(64 * most_waves(MT)) void k_matvec4(MatvecArgs q)
 {
     typedef Digits<G> D;
     constexpr int kBytes = G / 8;                                       // of weights of a lane and a set
-    __shared__ uint32_t digits[most_waves(MT)][D::total];
+    __shared__ uint32_t digits[MADE ? 1 : most_waves(MT)][MADE ? 1 : D::total];
     __shared__ u64 sums[most_waves(MT)][MT][16][2];
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64)), waves = blockDim.x / 64, lane = threadIdx.x % 64;
     const int n0 = blockIdx.x * 16, m0 = blockIdx.y * MT, kg = lane / 16;
     const u8* const w_row = q.w + (size_t)min(n0 + lane % 16, q.N - 1) * q.row_bytes;
     const int party = lane / 32, g8 = lane % 32;
     const u64* const x = q.x[party];
-    uint32_t* const mine = digits[wave];
+    uint32_t* const mine = digits[MADE ? 0 : wave];
     int64_t z[MT][4] = {};
-    for (int k0 = wave * kBlock; k0 < q.K; k0 += waves * kBlock) {
+    union Right { u64 words[8]; uint32_t d[16]; };                      // eight words to be made into digits, or a lane's digits
+    const auto right = [&](int block, int m) {
+        const int at_m = min(m0 + m, q.M - 1);
+        Right v;
+        if constexpr (MADE) {
+            const uint32_t* const from = q.digits + ((size_t)at_m * q.blocks + block) * 1024 + lane * 4;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) *reinterpret_cast<i32x4*>(v.d + i * 4) = *reinterpret_cast<const i32x4*>(from + i * 256);
+        } else {
+            const int k = block * kBlock + g8 * 8;
+            const u64* const row = x + (size_t)at_m * q.K;
+            if (block * kBlock + kBlock <= q.K)
+#pragma unroll
+                for (int j = 0; j < 8; j += 2) { const u64x2u t = *reinterpret_cast<const u64x2u*>(row + k + j); v.words[j] = t.x; v.words[j + 1] = t.y; }
+            else
+#pragma unroll
+                for (int j = 0; j < 8; ++j) { const u64 t = row[min(k + j, q.K - 1)]; v.words[j] = k + j < q.K ? t : 0; }
+        }
+        return v;
+    };
+    for (int block = wave; block < q.blocks; block += waves) {
+        const int k0 = block * kBlock;
+        Right next = right(block, 0);
         uint32_t w[8];                                                  // [set][kBytes / 4]
         int scale[D::sets][4];
 #pragma unroll
@@ -69,55 +121,47 @@ __global__ __launch_bounds__(64 * most_waves(MT)) void k_matvec4(MatvecArgs q)
 #pragma unroll
             for (int r = 0; r < 4; ++r) scale[s][r] = q.scales[(size_t)min(n0 + kg * 4 + r, q.N - 1) * q.groups + g];
         }
-        struct Eight { u64 w[8]; };
-        const auto words = [&](int m) {
-            const int k = k0 + g8 * 8;
-            const u64* const row = x + (size_t)min(m0 + m, q.M - 1) * q.K;
-            Eight v;
-            if (k0 + kBlock <= q.K)
-#pragma unroll
-                for (int j = 0; j < 8; j += 2) { const u64x2u t = *reinterpret_cast<const u64x2u*>(row + k + j); v.w[j] = t.x; v.w[j + 1] = t.y; }
-            else
-#pragma unroll
-                for (int j = 0; j < 8; ++j) { const u64 t = row[min(k + j, q.K - 1)]; v.w[j] = k + j < q.K ? t : 0; }
-            return v;
-        };
-        Eight next = words(0);
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-            const Eight v = next;
-            if (m + 1 < MT) next = words(m + 1);                        // one row ahead, and no further: registers
+            const Right v = next;
+            if (m + 1 < MT) next = right(block, m + 1);                 // one row ahead, and no further: registers
+            if constexpr (!MADE) {
 #pragma unroll
-            for (int odd = 0; odd < 2; ++odd) {
-                const u64 four[4] = { v.w[odd], v.w[2 + odd], v.w[4 + odd], v.w[6 + odd] };
-                uint32_t d[8];
-                digits_of_4(four, d);
+                for (int odd = 0; odd < 2; ++odd) {
+                    const u64 four[4] = { v.words[odd], v.words[2 + odd], v.words[4 + odd], v.words[6 + odd] };
+                    uint32_t d[8];
+                    digits_of_4(four, d);
 #pragma unroll
-                for (int p = 0; p < 8; ++p) mine[D::at(party, g8, odd) + p * D::dwords] = d[p];
+                    for (int p = 0; p < 8; ++p) mine[D::at(party, g8, odd) + p * D::dwords] = d[p];
+                }
+                __builtin_amdgcn_wave_barrier();                        // one wave: its LDS accesses are in order
             }
-            __builtin_amdgcn_wave_barrier();                            // one wave: its LDS accesses are in order
 #pragma unroll
             for (int s = 0; s < D::sets; ++s) {
-                const uint32_t* const at = mine + s * D::set + kg * D::row + lane % 16 * D::dwords;
+                uint32_t b[G == 128 ? 8 : D::dwords];
+                if constexpr (MADE) {
+#pragma unroll
+                    for (int i = 0; i < (int)(sizeof(b) / 4); ++i) b[i] = v.d[s * (sizeof(b) / 4) + i];
+                } else {
+                    const uint32_t* const at = mine + s * D::set + kg * D::row + lane % 16 * D::dwords;
+#pragma unroll
+                    for (int i = 0; i < (int)(sizeof(b) / 4); ++i) b[i] = at[i / 4 * 4 * D::row + i % 4];
+                }
                 i32x4 acc = { 0, 0, 0, 0 };
                 const auto low = [&](int i) { return (int)((w[i] << 4) & 0xf0f0f0f0u); };      // 16 q of the even columns, of the odd ones
                 const auto high = [&](int i) { return (int)(w[i] & 0xf0f0f0f0u); };
+                const auto four = [&](int i) { return i32x4{ (int)b[i], (int)b[i + 1], (int)b[i + 2], (int)b[i + 3] }; };
                 if constexpr (G == 128) {
-                    const i32x4 even = *reinterpret_cast<const i32x4*>(at), odd = *reinterpret_cast<const i32x4*>(at + 4 * D::row);
-                    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(i32x4{ low(s * 4), low(s * 4 + 1), low(s * 4 + 2), low(s * 4 + 3) }, even, acc, 0, 0, 0);
-                    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(i32x4{ high(s * 4), high(s * 4 + 1), high(s * 4 + 2), high(s * 4 + 3) }, odd, acc, 0, 0, 0);
-                } else if constexpr (G == 64) {
-                    const i32x4 b = *reinterpret_cast<const i32x4*>(at);
-                    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(i32x4{ low(s * 2), low(s * 2 + 1), high(s * 2), high(s * 2 + 1) }, b, acc, 0, 0, 0);
-                } else {
-                    const long b = *reinterpret_cast<const long*>(at);
-                    const long a = (long)((u64)(uint32_t)high(s) << 32 | (uint32_t)low(s));
-                    acc = __builtin_amdgcn_mfma_i32_16x16x32_i8(a, b, acc, 0, 0, 0);
-                }
+                    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(i32x4{ low(s * 4), low(s * 4 + 1), low(s * 4 + 2), low(s * 4 + 3) }, four(0), acc, 0, 0, 0);
+                    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(i32x4{ high(s * 4), high(s * 4 + 1), high(s * 4 + 2), high(s * 4 + 3) }, four(4), acc, 0, 0, 0);
+                } else if constexpr (G == 64)
+                    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(i32x4{ low(s * 2), low(s * 2 + 1), high(s * 2), high(s * 2 + 1) }, four(0), acc, 0, 0, 0);
+                else
+                    acc = __builtin_amdgcn_mfma_i32_16x16x32_i8((long)((u64)(uint32_t)high(s) << 32 | (uint32_t)low(s)), (long)((u64)b[1] << 32 | b[0]), acc, 0, 0, 0);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) z[m][r] += (int64_t)(acc[r] >> 4) * scale[s][r];   // the sixteenth is exact
             }
-            __builtin_amdgcn_sched_barrier(0);
+            if (MT > 1) __builtin_amdgcn_sched_barrier(0);
         }
     }
     // lane: column c = 8 party + digit of the product, rows 4 kg + r
@@ -139,22 +183,31 @@ __global__ __launch_bounds__(64 * most_waves(MT)) void k_matvec4(MatvecArgs q)
     }
 }
 
-template <int G, int MT> void launch(const MatvecArgs& q, hipStream_t st)
+template <int G, int MT, bool MADE> void launch(const MatvecArgs& q, hipStream_t st)
 {
-    const int blocks = (q.K + kBlock - 1) / kBlock, waves = blocks < most_waves(MT) ? blocks : most_waves(MT);
-    k_matvec4<G, MT><<<dim3((q.N + 15) / 16, (q.M + MT - 1) / MT), 64 * waves, 0, st>>>(q);
+    const int waves = q.blocks < most_waves(MT) ? q.blocks : most_waves(MT);
+    k_matvec4<G, MT, MADE><<<dim3((q.N + 15) / 16, (q.M + MT - 1) / MT), 64 * waves, 0, st>>>(q);
 }
 template <int G> void launch(const MatvecArgs& q, hipStream_t st)
 {
-    if (q.M == 1) launch<G, 1>(q, st);
-    else if (q.M == 2) launch<G, 2>(q, st);
-    else if (q.M <= 4) launch<G, 4>(q, st);
-    else launch<G, 8>(q, st);
+    if (digits_in_memory(q.M, q.K, q.N)) {
+        k_digits4<G><<<dim3((q.blocks + 3) / 4, q.M), 256, 0, st>>>(q);
+        launch<G, 8, true>(q, st);
+    }
+    else if (q.M == 1) launch<G, 1, false>(q, st);
+    else if (q.M == 2) launch<G, 2, false>(q, st);
+    else launch<G, 4, false>(q, st);
 }
 
 }  // namespace
 
 extern "C" {
+
+size_t mpc_matvec4_workspace_bytes(int M, int K, int N)
+{
+    if (M <= 0 || K <= 0 || N <= 0 || K > MPC_MAX_K_TOTAL || M > 65535 || !digits_in_memory(M, K, N)) return 0;
+    return (size_t)M * ((K + kBlock - 1) / kBlock) * 4096;
+}
 
 int mpc_matvec4(mpc_ctx* c, mpc_cshare x, const uint8_t* w, const int32_t* scales, mpc_share z,
                 int M, int K, int N, int group, int scale_bits)
@@ -173,6 +226,11 @@ int mpc_matvec4(mpc_ctx* c, mpc_cshare x, const uint8_t* w, const int32_t* scale
         if (overlap(z.p[i], out, w, (size_t)N * q.row_bytes) || overlap(z.p[i], out, scales, (size_t)N * q.groups * 4)) return MPC_EINVAL;
     }
     q.w = w; q.scales = scales; q.M = M; q.K = K; q.N = N; q.group = group; q.shift = scale_bits;
+    q.blocks = (K + kBlock - 1) / kBlock;
+    if (digits_in_memory(M, K, N)) {
+        if (!c->ws || c->ws_bytes < mpc_matvec4_workspace_bytes(M, K, N)) return MPC_ENOMEM;
+        q.digits = reinterpret_cast<uint32_t*>(c->ws);
+    }
     MPC_TRY(lane_first(c));
     if (group == 32) launch<32>(q, c->s[0]);
     else if (group == 64) launch<64>(q, c->s[0]);

@@ -95,7 +95,7 @@ EXPORTS = [
     "mpc_conv2d3_grad_x_workspace_bytes", "mpc_conv2d3_grad_w_workspace_bytes", "mpc_conv2d3_grad_x", "mpc_conv2d3_grad_w",
     "mpc_add3", "mpc_sub3", "mpc_mul3_workspace_bytes", "mpc_mul3", "mpc_relu3_backward", "mpc_maxpool3_signs",
     "mpc_maxpool3_backward_workspace_bytes", "mpc_maxpool3_backward",
-    "mpc_position_bias", "mpc_position_bias_grad", "mpc_matvec4", "mpc_linear_attention_workspace_bytes", "mpc_linear_attention",
+    "mpc_position_bias", "mpc_position_bias_grad", "mpc_matvec4", "mpc_matvec4_workspace_bytes", "mpc_linear_attention_workspace_bytes", "mpc_linear_attention",
     "mpc_linear_attention_step_workspace_bytes", "mpc_linear_attention_step",
 ]
 
@@ -219,6 +219,7 @@ def lib():
     L.mpc_maxpool3_backward.argtypes = [c_void_p] + [CShare3] * 10 + [c_int] * 4
     L.mpc_position_bias.argtypes = [c_void_p, CShare, CShare, c_void_p, CShare] + [c_int] * 5
     L.mpc_position_bias_grad.argtypes = [c_void_p, CShare, c_void_p, CShare, CShare] + [c_int] * 5
+    L.mpc_matvec4_workspace_bytes.argtypes = [c_int] * 3; L.mpc_matvec4_workspace_bytes.restype = c_size_t
     L.mpc_matvec4.argtypes = [c_void_p, CShare, c_void_p, c_void_p, CShare] + [c_int] * 5
     L.mpc_linear_attention_workspace_bytes.argtypes = [c_int] * 5; L.mpc_linear_attention_workspace_bytes.restype = c_size_t
     L.mpc_linear_attention.argtypes = [c_void_p] + [CShare] * 3 + [Strides] * 3 + [c_void_p, POINTER(AttentionMaterial), CShare, CShare, Strides, CShare] + [c_int] * 5
@@ -1021,6 +1022,9 @@ class Lane:
         xs, zs = _dense_share(x, (M, K), self.device, "x"), _dense_share(out, (M, N), self.device, "out")
         wp = _dense(w, (N, -(-K // 32) * 16), torch.uint8, self.device, "w")
         sp = _dense(scales, (N, -(-K // group)), torch.int32, self.device, "scales")
+        need = lib().mpc_matvec4_workspace_bytes(M, K, N)
+        if need > self._ws_bytes:
+            self.reserve(need)
         self._check(lib().mpc_matvec4(self._h, xs, wp, sp, zs, M, K, N, group, scale_bits))
         return out
 

@@ -141,6 +141,7 @@ for n in ("mpc_linear_attention_workspace_bytes", "mpc_linear_attention_step_wor
 P = c_void_p
 lib.mpc_position_bias.argtypes = [P, Share, Share, P, Share] + [c_int] * 5
 lib.mpc_position_bias_grad.argtypes = [P, Share, P, Share, Share] + [c_int] * 5
+lib.mpc_matvec4_workspace_bytes.restype = c_size_t
 lib.mpc_matvec4.argtypes = [P, Share, P, P, Share] + [c_int] * 5
 lib.mpc_linear_attention.argtypes = [P, Share, Share, Share, Strides, Strides, Strides, P, P, Share, Share, Strides, Share] + [c_int] * 5
 lib.mpc_linear_attention_step.argtypes = [P, Share, Share, Share, Strides, Strides, Strides, P, P, Share, Share, Strides, Share] + [c_int] * 4
@@ -177,6 +178,8 @@ result["prompt"] = [prompt(), prompt(state=none), prompt(out=none), prompt(state
                     prompt(dv=0), prompt(dk=129), prompt(dv=200), prompt(ws=False), prompt(sq=Strides(-1, 8, 8)), prompt(so=Strides(0, 18, 6)), prompt(so=Strides(1260, 18, 5)),
                     prompt(so=Strides(1259, 18, 6)), prompt(q=x, o=x), prompt(q=x, out=x), prompt(state=x, o=x), prompt(o=x, out=x), prompt(state=x, out=shifted),
                     prompt(B=1 << 20, H=1 << 12)]
+lib.mpc_ctx_set_workspace(ctx, array(4096), 4096)
+result["matvec4 without room"] = [mv(M=16, K=4096, N=4096), mv(M=16, K=4096, N=100)]
 result["drops"] = [prompt(drop=i) for i in range(10)]
 def step(q=None, so=None, state=None, o=None, out=None, ws=True, B=B, H=H, dk=dk, dv=dv, drop=None):
     need = lib.mpc_linear_attention_step_workspace_bytes(B, H, dk, dv)
@@ -208,6 +211,7 @@ def test_refusals(tmp_path):
     assert r["grad"] == [0, 0] + [E] * 5 + [R] + [E] * 3
     assert r["matvec4"] == [0] * 6 + [E] * 15 + [R, R] + [E] * 3
     assert r["prompt"] == [0] * 7 + [E] * 11 + [R, R, M] + [E] * 9 + [R]
+    assert r["matvec4 without room"] == [M, 0]
     assert r["drops"] == [E] * 10 and r["step_drops"] == [E] * 6
     assert r["step"] == [0] * 4 + [E] * 5 + [R, M] + [E] * 5
     assert r["frac"] == [R, R] and r["null"] == [E, E] and r["launched by refused calls"] == []
@@ -217,5 +221,7 @@ def test_workspace_queries_refuse():
     from paper_2209_13643_amd import mpc
     L = mpc.lib()
     assert L.mpc_linear_attention_workspace_bytes(1, 0, 1, 8, 8) == 0 and L.mpc_linear_attention_workspace_bytes(1, 1, 1, 129, 8) == 0
+    assert L.mpc_matvec4_workspace_bytes(0, 1 << 14, 1 << 14) == 0 and L.mpc_matvec4_workspace_bytes(1, 1 << 14, 1 << 14) == 0
+    assert L.mpc_matvec4_workspace_bytes(16, 4100, 4096) == 16 * 17 * 4096
     assert L.mpc_linear_attention_step_workspace_bytes(0, 1, 8, 8) == 0 and L.mpc_linear_attention_step_workspace_bytes(1, 1, 8, 8) > 0
     assert L.mpc_linear_attention_workspace_bytes(1, 65, 1, 8, 8) > L.mpc_linear_attention_workspace_bytes(1, 64, 1, 8, 8) > 0

@@ -162,6 +162,22 @@ def test_matvec4(mpc, lane, attention, M, K, N, group, bits):
     equal(mpc, z, plain.matvec4(x, q, scales, group, bits))
 
 
+@pytest.mark.parametrize("M,K,N,group", [(9, 4100, 3700, 32), (8, 4097, 4100, 64), (17, 2050, 3900, 128), (5, 10241, 2630, 1024)])
+def test_matvec4_many_rows(mpc, lane, attention, M, K, N, group):
+    """Products whose digits are made once for all workgroups, on a workspace of exactly the size of the query."""
+    print(f"matvec4 {M}x{K}x{N} group {group}", flush=True)
+    rng = np.random.default_rng(M)
+    q, scales, x = rng.integers(-8, 8, (N, K)), rng.integers(-(1 << 31), 1 << 31, (N, -(-K // group))).astype(np.int32), inputs.masks(rng, M, K)
+    need = mpc.lib().mpc_matvec4_workspace_bytes(M, K, N)
+    assert need > 0
+    from test_gpu_workspace_bounds import Guarded
+    g = Guarded(mpc, need)
+    g.lane._ws_bytes = need                                  # what the library was told: not to be grown
+    z = g.lane.matvec4(dev(mpc, x), attention.pack_weights4(torch.from_numpy(q)).cuda(), mpc.to_device(scales), group, 20)
+    g.check()
+    equal(mpc, z, plain.matvec4(x, q, scales, group, 20))
+
+
 def test_matvec4_extreme_weights(mpc, lane, attention):
     """Every weight -8, every scale -2^31 and words whose digits are all -128: the largest sums there are."""
     M, K, N = 2, 20000, 3
