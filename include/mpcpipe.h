@@ -576,16 +576,23 @@ int mpc_matvec4(mpc_ctx* ctx, mpc_cshare x, const uint8_t* w, const int32_t* sca
 #define MPC_ATTENTION_MAX_D 128
 #define MPC_ATTENTION_MAX_TOKEN_STRIDE 4194303     /* of q, k, v of a prompt, in words */
 typedef struct { int64_t batch, token, head; } mpc_strides;
+typedef struct {
+    mpc_cshare q, k, v;
+    mpc_strides sq, sk, sv;          /* a step has no use for the tokens' */
+    const int32_t* decay;
+    mpc_cshare state;
+    mpc_share o;
+    mpc_strides so;
+    mpc_share state_out;
+} mpc_attention_operands;
 typedef struct { mpc_cshare a_q, a_k, a_qd, a_kd, a_v, a_w, a_s, c_p, c_u, c_o; } mpc_attention_material;
 typedef struct { mpc_cshare a_q, a_k, a_v, a_s, c_u, c_o; } mpc_attention_step_material;
 size_t mpc_linear_attention_workspace_bytes(int B, int T, int H, int dk, int dv);
-int mpc_linear_attention(mpc_ctx* ctx, mpc_cshare q, mpc_cshare k, mpc_cshare v, mpc_strides sq, mpc_strides sk, mpc_strides sv,
-                         const int32_t* decay, const mpc_attention_material* mat, mpc_cshare state, mpc_share o, mpc_strides so,
-                         mpc_share state_out, int B, int T, int H, int dk, int dv);
+int mpc_linear_attention(mpc_ctx* ctx, const mpc_attention_operands* x, const mpc_attention_material* mat,
+                         int B, int T, int H, int dk, int dv);
 size_t mpc_linear_attention_step_workspace_bytes(int B, int H, int dk, int dv);
-int mpc_linear_attention_step(mpc_ctx* ctx, mpc_cshare q, mpc_cshare k, mpc_cshare v, mpc_strides sq, mpc_strides sk, mpc_strides sv,
-                              const int32_t* decay, const mpc_attention_step_material* mat, mpc_cshare state, mpc_share o,
-                              mpc_strides so, mpc_share state_out, int B, int H, int dk, int dv);
+int mpc_linear_attention_step(mpc_ctx* ctx, const mpc_attention_operands* x, const mpc_attention_step_material* mat,
+                              int B, int H, int dk, int dv);
 
 /* ------------------------------------------ three parties (Sec. 3.3, Sec. 5.6) */
 

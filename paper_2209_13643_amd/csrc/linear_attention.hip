@@ -588,14 +588,14 @@ size_t mpc_linear_attention_step_workspace_bytes(int B, int H, int dk, int dv)
     return shape_ok(nullptr, B, 1, H, dk, dv) == MPC_OK ? (size_t)kStepBoxes * 2 * kStepBoxWords * 8 : 0;
 }
 
-int mpc_linear_attention(mpc_ctx* c, mpc_cshare q, mpc_cshare k, mpc_cshare v, mpc_strides sq, mpc_strides sk, mpc_strides sv,
-                         const int32_t* decay, const mpc_attention_material* m, mpc_cshare state, mpc_share o, mpc_strides so,
-                         mpc_share state_out, int B, int T, int H, int dk, int dv)
+int mpc_linear_attention(mpc_ctx* c, const mpc_attention_operands* x, const mpc_attention_material* m, int B, int T, int H, int dk, int dv)
 {
-    if (!c || !decay || !m || !both(q) || !both(k) || !both(v) || !both(seen(o))) return MPC_EINVAL;
+    if (!c || !x || !m) return MPC_EINVAL;
+    const auto [q, k, v, sq, sk, sv, decay, state, o, so, state_out] = *x;
+    if (!decay || !both(q) || !both(k) || !both(v) || !both(seen(o))) return MPC_EINVAL;
     if (!state.p[0] != !state.p[1] || !state_out.p[0] != !state_out.p[1]) return MPC_EINVAL;
     const mpc_cshare* const mats[] = { &m->a_q, &m->a_k, &m->a_qd, &m->a_kd, &m->a_v, &m->a_w, &m->a_s, &m->c_p, &m->c_u, &m->c_o };
-    for (const mpc_cshare* x : mats) if (!both(*x)) return MPC_EINVAL;
+    for (const mpc_cshare* w : mats) if (!both(*w)) return MPC_EINVAL;
     MPC_TRY(shape_ok(c, B, T, H, dk, dv));
     if (!strides_in(sq) || !strides_in(sk) || !strides_in(sv) || !strides_out(so, B, T, H, dv)) return MPC_EINVAL;
     if (far_tokens(sq) || far_tokens(sk) || far_tokens(sv)) return MPC_ERANGE;
@@ -640,13 +640,13 @@ int mpc_linear_attention(mpc_ctx* c, mpc_cshare q, mpc_cshare k, mpc_cshare v, m
     return lane_fanout(c);
 }
 
-int mpc_linear_attention_step(mpc_ctx* c, mpc_cshare q, mpc_cshare k, mpc_cshare v, mpc_strides sq, mpc_strides sk, mpc_strides sv,
-                              const int32_t* decay, const mpc_attention_step_material* m, mpc_cshare state, mpc_share o, mpc_strides so,
-                              mpc_share state_out, int B, int H, int dk, int dv)
+int mpc_linear_attention_step(mpc_ctx* c, const mpc_attention_operands* x, const mpc_attention_step_material* m, int B, int H, int dk, int dv)
 {
-    if (!c || !decay || !m || !both(q) || !both(k) || !both(v) || !both(state) || !both(seen(o)) || !both(seen(state_out))) return MPC_EINVAL;
+    if (!c || !x || !m) return MPC_EINVAL;
+    auto [q, k, v, sq, sk, sv, decay, state, o, so, state_out] = *x;
+    if (!decay || !both(q) || !both(k) || !both(v) || !both(state) || !both(seen(o)) || !both(seen(state_out))) return MPC_EINVAL;
     const mpc_cshare* const mats[] = { &m->a_q, &m->a_k, &m->a_v, &m->a_s, &m->c_u, &m->c_o };
-    for (const mpc_cshare* x : mats) if (!both(*x)) return MPC_EINVAL;
+    for (const mpc_cshare* w : mats) if (!both(*w)) return MPC_EINVAL;
     MPC_TRY(shape_ok(c, B, 1, H, dk, dv));
     sq.token = sk.token = sv.token = so.token = 0;
     if (!strides_in(sq) || !strides_in(sk) || !strides_in(sv) || !strides_out(so, B, 1, H, dv)) return MPC_EINVAL;

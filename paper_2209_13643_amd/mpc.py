@@ -48,22 +48,8 @@ class Relu3Material(ctypes.Structure):
                 ("rb", _P8 * 3), ("ra", CShare3), ("ma", CShare3), ("mb", CShare3), ("mc", CShare3)]
 
 
-class Strides(ctypes.Structure):
-    _fields_ = [("batch", ctypes.c_int64), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
-
-
 _ATTENTION_MASKS = ("a_q", "a_k", "a_qd", "a_kd", "a_v", "a_w", "a_s", "c_p", "c_u", "c_o")
 _STEP_MASKS = ("a_q", "a_k", "a_v", "a_s", "c_u", "c_o")
-
-
-class AttentionMaterial(ctypes.Structure):
-    _fields_ = [(n, CShare) for n in _ATTENTION_MASKS]
-
-
-class AttentionStepMaterial(ctypes.Structure):
-    _fields_ = [(n, CShare) for n in _STEP_MASKS]
-
-
 ATTENTION_CHUNK, ATTENTION_MAX_D, MAX_BUCKETS = 64, 128, 4096
 
 N_AND_TRIPLES3 = 13
@@ -222,9 +208,9 @@ def lib():
     L.mpc_matvec4_workspace_bytes.argtypes = [c_int] * 3; L.mpc_matvec4_workspace_bytes.restype = c_size_t
     L.mpc_matvec4.argtypes = [c_void_p, CShare, c_void_p, c_void_p, CShare] + [c_int] * 5
     L.mpc_linear_attention_workspace_bytes.argtypes = [c_int] * 5; L.mpc_linear_attention_workspace_bytes.restype = c_size_t
-    L.mpc_linear_attention.argtypes = [c_void_p] + [CShare] * 3 + [Strides] * 3 + [c_void_p, POINTER(AttentionMaterial), CShare, CShare, Strides, CShare] + [c_int] * 5
+    L.mpc_linear_attention.argtypes = [c_void_p, ctypes.c_char_p, ctypes.c_char_p] + [c_int] * 5
     L.mpc_linear_attention_step_workspace_bytes.argtypes = [c_int] * 4; L.mpc_linear_attention_step_workspace_bytes.restype = c_size_t
-    L.mpc_linear_attention_step.argtypes = [c_void_p] + [CShare] * 3 + [Strides] * 3 + [c_void_p, POINTER(AttentionStepMaterial), CShare, CShare, Strides, CShare] + [c_int] * 4
+    L.mpc_linear_attention_step.argtypes = [c_void_p, ctypes.c_char_p, ctypes.c_char_p] + [c_int] * 4
     _lib = L
     return L
 
@@ -316,46 +302,58 @@ def _material3(mat: dict, n: int, packed: bool = False) -> Relu3Material:
     return Relu3Material.from_buffer_copy(_pack_material3(*addresses))
 
 
-def _dense(t, shape, dtype, device, name):
-    """Checked device address of a dense tensor."""
-    if t.shape != shape or t.dtype is not dtype or t.device != device or not t.is_contiguous():
-        raise ValueError(f"'{name}': contiguous {dtype} tensor of shape {list(shape)} on {device} expected, "
+# The attention and public-weight calls: addresses are checked where they are read, and a call's operands and material travel as
+# one packed structure each (mpc_attention_operands, mpc_attention_material) instead of a ctypes object for every share: one token's
+# call names 24 tensors.
+_pack_operands = struct.Struct("6Q9qQ4Q3q2Q").pack
+_pack_prompt, _pack_step = struct.Struct("20Q").pack, struct.Struct("12Q").pack
+_int64 = torch.int64
+
+
+def _dense(t, shape, dtype, index, name):
+    """Checked device address of a dense tensor on device `index`."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"'{name}': contiguous {dtype} tensor of shape {list(shape)} on device {index} expected, "
                          f"got {t.dtype} {list(t.shape)} on {t.device}")
-    _noted().append(t)
     return t.data_ptr()
 
 
-def _dense_share(pair, shape, device, name):
+def _two(pair, name):
     if len(pair) != 2:
         raise ValueError(f"'{name}': a sharing is a pair of tensors")
-    return CShare.from_buffer_copy(_pack2(_dense(pair[0], shape, torch.int64, device, name), _dense(pair[1], shape, torch.int64, device, name)))
+    return pair
 
 
-def _heads_share(pair, shape, device, name):
-    """Addresses and strides of a sharing of [B, (T,) H, d]; the last axis is dense, the others lie as they lie."""
-    if len(pair) != 2:
-        raise ValueError(f"'{name}': a sharing is a pair of tensors")
-    a, b = pair
+def _dense_share(pair, shape, index, name):
+    a, b = _two(pair, name)
+    return CShare.from_buffer_copy(_pack2(_dense(a, shape, _int64, index, name), _dense(b, shape, _int64, index, name)))
+
+
+def _heads(pair, shape, index, name):
+    """(addresses, strides) of a sharing of [B, (T,) H, d]; the last axis is dense, the others lie as they lie."""
+    a, b = _two(pair, name)
     st = a.stride()
-    for t in pair:
-        if t.shape != shape or t.dtype is not torch.int64 or t.device != device or t.stride() != st or (st[-1] != 1 and shape[-1] != 1):
-            raise ValueError(f"'{name}': int64 tensors of shape {list(shape)} on {device}, dense in the last axis and with the same "
-                             f"strides for both shares expected, got {t.dtype} {list(t.shape)} strides {t.stride()} on {t.device}")
-    _noted().extend(pair)
-    strides = Strides(st[0], st[1], st[2]) if len(shape) == 4 else Strides(st[0], 0, st[1])
-    return CShare.from_buffer_copy(_pack2(a.data_ptr(), b.data_ptr())), strides
+    if (a.dtype is not _int64 or b.dtype is not _int64 or a.shape != shape or b.shape != shape or a.get_device() != index
+            or b.get_device() != index or b.stride() != st or (st[-1] != 1 and shape[-1] != 1)):
+        raise ValueError(f"'{name}': int64 tensors of shape {list(shape)} on device {index}, dense in the last axis and with the same "
+                         f"strides for both shares expected, got {[(t.dtype, list(t.shape), t.stride(), str(t.device)) for t in pair]}")
+    return (a.data_ptr(), b.data_ptr()), (st[:3] if len(st) == 4 else (st[0], 0, st[1]))
 
 
-def _attention_material(struct_type, names, mat, shapes, device):
-    missing = [n for n in names if n not in mat]
-    if missing:
-        raise ValueError(f"material lacks {missing}")
-    words = []
+def _attention_material(names, mat, words, index, keep):
+    """Addresses of a material's dense arrays, by the number of their words; the tensors are added to `keep`."""
+    out = []
     for n in names:
-        if len(mat[n]) != 2:
-            raise ValueError(f"material '{n}': a sharing is a pair of tensors")
-        words += [_dense(t, shapes[n], torch.int64, device, n) for t in mat[n]]
-    return struct_type.from_buffer_copy(struct.pack(f"{len(words)}Q", *words))
+        if n not in mat:
+            raise ValueError(f"material lacks '{n}'")
+        pair, want = _two(mat[n], n), words[n]
+        for t in pair:
+            if t.numel() != want or t.dtype is not _int64 or t.get_device() != index or not t.is_contiguous():
+                raise ValueError(f"material '{n}': {want} dense int64 words per party on device {index} expected, "
+                                 f"got {t.dtype} {list(t.shape)} on {t.device}")
+            out.append(t.data_ptr())
+        keep += pair
+    return out
 
 
 def to_device(arr, device="cuda:0"):
@@ -445,6 +443,7 @@ class Lane:
         if not torch.cuda.is_available():
             raise RuntimeError("mpcpipe needs a GPU: no HIP device is visible")
         self.device = torch.device("cuda", device)
+        self._index = device
         self._h = c_void_p()
         self._handed = set()         # streams whose handles the caller has
         self._pending = []           # tensors the enqueued calls still use (see _marshalled); released by sync()
@@ -988,44 +987,48 @@ class Lane:
     def position_bias(self, scores, table, buckets, out=None):
         """scores [B, H, Tq, Tk] + table [n, H] at the public bucket of every pair: buckets int32 [Tq + Tk - 1], entry
         j - i + Tq - 1 of query i and key j; an entry outside [0, n) masks its pairs (zero).  out may be scores."""
-        B, H, Tq, Tk = scores[0].shape
+        shape, at = scores[0].shape, self._index
+        B, H, Tq, Tk = shape
         n = table[0].shape[0]
         out = out if out is not None else (torch.empty_like(scores[0]), torch.empty_like(scores[1]))
-        shape = scores[0].shape
-        s, t, o = (_dense_share(scores, shape, self.device, "scores"), _dense_share(table, (n, H), self.device, "table"),
-                   _dense_share(out, shape, self.device, "out"))
-        m = _dense(buckets, (Tq + Tk - 1,), torch.int32, self.device, "buckets")
+        s, t, o = _dense_share(scores, shape, at, "scores"), _dense_share(table, (n, H), at, "table"), _dense_share(out, shape, at, "out")
+        m = _dense(buckets, (Tq + Tk - 1,), torch.int32, at, "buckets")
+        self._pending += (*scores, *table, buckets, *out)
         self._check(lib().mpc_position_bias(self._h, s, t, m, o, B, H, Tq, Tk, n))
         return out
 
     def position_bias_grad(self, g, buckets, n_buckets, out=None, scores_out=None):
         """Gradient of position_bias for its output's g: (table's [n_buckets, H], scores').  The scores' gradient is g with
         zeros at masked pairs; it is written to scores_out (may be g), or not at all if that is None."""
-        B, H, Tq, Tk = g[0].shape
+        shape, at = g[0].shape, self._index
+        B, H, Tq, Tk = shape
         if out is None:
-            out = tuple(torch.empty((n_buckets, H), dtype=torch.int64, device=self.device) for _ in range(2))
-        shape = g[0].shape
-        s, o = _dense_share(g, shape, self.device, "g"), _dense_share(out, (n_buckets, H), self.device, "out")
-        so = _dense_share(scores_out, shape, self.device, "scores_out") if scores_out is not None else CShare()
-        m = _dense(buckets, (Tq + Tk - 1,), torch.int32, self.device, "buckets")
+            out = tuple(torch.empty((n_buckets, H), dtype=_int64, device=self.device) for _ in range(2))
+        s, o = _dense_share(g, shape, at, "g"), _dense_share(out, (n_buckets, H), at, "out")
+        so = _dense_share(scores_out, shape, at, "scores_out") if scores_out is not None else CShare()
+        m = _dense(buckets, (Tq + Tk - 1,), torch.int32, at, "buckets")
+        self._pending += (*g, buckets, *out, *(scores_out or ()))
         self._check(lib().mpc_position_bias_grad(self._h, s, m, o, so, B, H, Tq, Tk, n_buckets))
         return out, scores_out
 
     def matvec4(self, x, w, scales, group, scale_bits=16, out=None):
         """x [M, K] times public 4-bit weights: w uint8 [N, 16 ceil(K / 32)] (attention.pack_weights4), scales int32
         [N, ceil(K / group)] with scale_bits fraction bits.  z [M, N] in x's fixed point."""
-        M, K = x[0].shape
+        shape, at = x[0].shape, self._index
+        M, K = shape
         N = w.shape[0]
-        out = out if out is not None else tuple(torch.empty((M, N), dtype=torch.int64, device=self.device) for _ in range(2))
+        out = out if out is not None else tuple(torch.empty((M, N), dtype=_int64, device=self.device) for _ in range(2))
         if group <= 0:
             raise ValueError(f"group: a positive number of columns expected, got {group}")
-        xs, zs = _dense_share(x, (M, K), self.device, "x"), _dense_share(out, (M, N), self.device, "out")
-        wp = _dense(w, (N, -(-K // 32) * 16), torch.uint8, self.device, "w")
-        sp = _dense(scales, (N, -(-K // group)), torch.int32, self.device, "scales")
-        need = lib().mpc_matvec4_workspace_bytes(M, K, N)
+        xs, zs = _dense_share(x, shape, at, "x"), _dense_share(out, (M, N), at, "out")
+        wp = _dense(w, (N, (K + 31) // 32 * 16), torch.uint8, at, "w")
+        sp = _dense(scales, (N, -(-K // group)), torch.int32, at, "scales")
+        L = lib()
+        need = L.mpc_matvec4_workspace_bytes(M, K, N)
         if need > self._ws_bytes:
             self.reserve(need)
-        self._check(lib().mpc_matvec4(self._h, xs, wp, sp, zs, M, K, N, group, scale_bits))
+        self._pending += (*x, w, scales, *out)
+        self._check(L.mpc_matvec4(self._h, xs, wp, sp, zs, M, K, N, group, scale_bits))
         return out
 
     def linear_attention(self, q, k, v, decay, mat, state=None, out=None, state_out=None):
@@ -1034,42 +1037,41 @@ class Lane:
         [B, H, dk, dv] before the first token (None: zero).  Returns (o [B, T, H, dv], state after the last token);
         state_out may be state."""
         B, T, H, dk = q[0].shape
-        dv = v[0].shape[-1]
-        dev, BH, nc = self.device, B * H, -(-T // ATTENTION_CHUNK)
-        empty = lambda *shape: tuple(torch.empty(shape, dtype=torch.int64, device=dev) for _ in range(2))
-        out = out if out is not None else empty(B, T, H, dv)
-        state_out = state_out if state_out is not None else empty(B, H, dk, dv)
-        self.reserve(lib().mpc_linear_attention_workspace_bytes(B, T, H, dk, dv))
-        (qs, sq), (ks, sk) = _heads_share(q, (B, T, H, dk), dev, "q"), _heads_share(k, (B, T, H, dk), dev, "k")
-        (vs, sv), (os_, so) = _heads_share(v, (B, T, H, dv), dev, "v"), _heads_share(out, (B, T, H, dv), dev, "out")
-        rows, cells = (BH, T, dk), (BH, nc, dk, dv)
-        shapes = dict(a_q=rows, a_k=rows, a_qd=rows, a_kd=rows, a_v=(BH, T, dv), a_w=(BH, T, ATTENTION_CHUNK), a_s=cells,
-                      c_p=(BH, T, ATTENTION_CHUNK), c_u=cells, c_o=(BH, T, dv))
-        m = _attention_material(AttentionMaterial, _ATTENTION_MASKS, mat, shapes, dev)
-        st = _dense_share(state, (B, H, dk, dv), dev, "state") if state is not None else CShare()
-        sn = _dense_share(state_out, (B, H, dk, dv), dev, "state_out")
-        d = _dense(decay, (H, ATTENTION_CHUNK + 1), torch.int32, dev, "decay")
-        self._check(lib().mpc_linear_attention(self._h, qs, ks, vs, sq, sk, sv, d, byref(m), st, os_, so, sn, B, T, H, dk, dv))
-        return out, state_out
+        dv, nc = v[0].shape[-1], -(-T // ATTENTION_CHUNK)
+        rows, tok, cells = B * H * T, B * H * T * ATTENTION_CHUNK, B * H * nc * dk * dv
+        words = dict(a_q=rows * dk, a_k=rows * dk, a_qd=rows * dk, a_kd=rows * dk, a_v=rows * dv, a_w=tok, a_s=cells, c_p=tok, c_u=cells,
+                     c_o=rows * dv)
+        return self._attend(q, k, v, decay, mat, state, out, state_out, (B, T, H), dk, dv, words)
 
     def linear_attention_step(self, q, k, v, decay, mat, state, out=None, state_out=None):
         """One token of linear_attention: q, k [B, H, dk], v [B, H, dv], state [B, H, dk, dv]; mat as
         dealer.attention_step_material deals it.  Returns (o [B, H, dv], new state); state_out may be state."""
         B, H, dk = q[0].shape
-        dv = v[0].shape[-1]
-        dev = self.device
-        empty = lambda *shape: tuple(torch.empty(shape, dtype=torch.int64, device=dev) for _ in range(2))
-        out = out if out is not None else empty(B, H, dv)
-        state_out = state_out if state_out is not None else empty(B, H, dk, dv)
-        self.reserve(lib().mpc_linear_attention_step_workspace_bytes(B, H, dk, dv))
-        (qs, sq), (ks, sk) = _heads_share(q, (B, H, dk), dev, "q"), _heads_share(k, (B, H, dk), dev, "k")
-        (vs, sv), (os_, so) = _heads_share(v, (B, H, dv), dev, "v"), _heads_share(out, (B, H, dv), dev, "out")
+        dv, n = v[0].shape[-1], B * H
+        if state is None:
+            raise ValueError("a step goes on from a state")
+        words = dict(a_q=n * dk, a_k=n * dk, a_v=n * dv, a_s=n * dk * dv, c_u=n * dk * dv, c_o=n * dv)
+        return self._attend(q, k, v, decay, mat, state, out, state_out, (B, H), dk, dv, words)
+
+    def _attend(self, q, k, v, decay, mat, state, out, state_out, lead, dk, dv, words):
+        B, H, at, L, prompt = lead[0], lead[-1], self._index, lib(), len(lead) == 3
         cell = (B, H, dk, dv)
-        shapes = dict(a_q=(B, H, dk), a_k=(B, H, dk), a_v=(B, H, dv), a_s=cell, c_u=cell, c_o=(B, H, dv))
-        m = _attention_material(AttentionStepMaterial, _STEP_MASKS, mat, shapes, dev)
-        st, sn = _dense_share(state, cell, dev, "state"), _dense_share(state_out, cell, dev, "state_out")
-        d = _dense(decay, (H, ATTENTION_CHUNK + 1), torch.int32, dev, "decay")
-        self._check(lib().mpc_linear_attention_step(self._h, qs, ks, vs, sq, sk, sv, d, byref(m), st, os_, so, sn, B, H, dk, dv))
+        out = out if out is not None else tuple(torch.empty((*lead, dv), dtype=_int64, device=self.device) for _ in range(2))
+        state_out = state_out if state_out is not None else tuple(torch.empty(cell, dtype=_int64, device=self.device) for _ in range(2))
+        (qs, sq), (ks, sk) = _heads(q, (*lead, dk), at, "q"), _heads(k, (*lead, dk), at, "k")
+        (vs, sv), (os_, so) = _heads(v, (*lead, dv), at, "v"), _heads(out, (*lead, dv), at, "out")
+        st = [_dense(t, cell, _int64, at, "state") for t in _two(state, "state")] if state is not None else (0, 0)
+        sn = [_dense(t, cell, _int64, at, "state_out") for t in _two(state_out, "state_out")]
+        d = _dense(decay, (H, ATTENTION_CHUNK + 1), torch.int32, at, "decay")
+        keep = [*q, *k, *v, decay, *out, *state_out, *(state or ())]
+        m = _attention_material(_ATTENTION_MASKS if prompt else _STEP_MASKS, mat, words, at, keep)
+        need = (L.mpc_linear_attention_workspace_bytes if prompt else L.mpc_linear_attention_step_workspace_bytes)(*lead, dk, dv)
+        if need == 0 or need > self._ws_bytes:
+            self.reserve(need)
+        self._pending += keep
+        x = _pack_operands(*qs, *ks, *vs, *sq, *sk, *sv, d, *st, *os_, *so, *sn)
+        self._check(L.mpc_linear_attention(self._h, x, _pack_prompt(*m), *lead, dk, dv) if prompt else
+                    L.mpc_linear_attention_step(self._h, x, _pack_step(*m), *lead, dk, dv))
         return out, state_out
 
     def ring_matmul(self, L, R):

@@ -132,6 +132,9 @@ def test_decay_powers():
 REFUSALS = r'''
 class Strides(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int64), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
+class Operands(ctypes.Structure):
+    _fields_ = [("q", Share), ("k", Share), ("v", Share), ("sq", Strides), ("sk", Strides), ("sv", Strides), ("decay", c_void_p), ("state", Share), ("o", Share),
+                ("so", Strides), ("state_out", Share)]
 class Material(ctypes.Structure):
     _fields_ = [("s", Share * 10)]
 class StepMaterial(ctypes.Structure):
@@ -143,8 +146,8 @@ lib.mpc_position_bias.argtypes = [P, Share, Share, P, Share] + [c_int] * 5
 lib.mpc_position_bias_grad.argtypes = [P, Share, P, Share, Share] + [c_int] * 5
 lib.mpc_matvec4_workspace_bytes.restype = c_size_t
 lib.mpc_matvec4.argtypes = [P, Share, P, P, Share] + [c_int] * 5
-lib.mpc_linear_attention.argtypes = [P, Share, Share, Share, Strides, Strides, Strides, P, P, Share, Share, Strides, Share] + [c_int] * 5
-lib.mpc_linear_attention_step.argtypes = [P, Share, Share, Share, Strides, Strides, Strides, P, P, Share, Share, Strides, Share] + [c_int] * 4
+lib.mpc_linear_attention.argtypes = [P, P, P] + [c_int] * 5
+lib.mpc_linear_attention_step.argtypes = [P, P, P] + [c_int] * 4
 def share(nbytes): return Share((c_void_p * 2)(array(nbytes), array(nbytes)))
 none, half = Share(), Share((c_void_p * 2)(array(64), None))
 big = 1 << 24
@@ -171,8 +174,9 @@ def prompt(q=None, sq=None, so=None, m=None, state=None, o=None, out=None, decay
     need = lib.mpc_linear_attention_workspace_bytes(B, T, H, dk, dv)
     lib.mpc_ctx_set_workspace(ctx, array(max(need, 1)), need - (0 if ws else 1) if need else 0)
     mat = Material((Share * 10)(*[none if i == drop else share(big) for i in range(10)]))
-    return lib.mpc_linear_attention(ctx, q or share(big), share(big), share(big), sq or nat(T, dk), nat(T, dk), nat(T, dv), array(big) if decay is None else decay or None,
-        ctypes.byref(mat) if m is None else None, share(big) if state is None else state, o or share(big), so or nat(T, dv), share(big) if out is None else out, B, T, H, dk, dv)
+    x = Operands(q or share(big), share(big), share(big), sq or nat(T, dk), nat(T, dk), nat(T, dv), array(big) if decay is None else decay or None,
+                 share(big) if state is None else state, o or share(big), so or nat(T, dv), share(big) if out is None else out)
+    return lib.mpc_linear_attention(ctx, ctypes.byref(x), ctypes.byref(mat) if m is None else None, B, T, H, dk, dv)
 result["prompt"] = [prompt(), prompt(state=none), prompt(out=none), prompt(state=x, out=x), prompt(sq=Strides(0, 0, 0)), prompt(T=1), prompt(dk=128, dv=128),
                     prompt(q=none), prompt(m=0), prompt(decay=0), prompt(state=half), prompt(out=half), prompt(o=none), prompt(B=0), prompt(T=0), prompt(H=0), prompt(dk=0),
                     prompt(dv=0), prompt(dk=129), prompt(dv=200), prompt(ws=False), prompt(sq=Strides(-1, 8, 8)), prompt(so=Strides(0, 18, 6)), prompt(so=Strides(1260, 18, 5)),
@@ -186,8 +190,9 @@ def step(q=None, so=None, state=None, o=None, out=None, ws=True, B=B, H=H, dk=dk
     lib.mpc_ctx_set_workspace(ctx, array(max(need, 1)), need - (0 if ws else 1) if need else 0)
     mat = StepMaterial((Share * 6)(*[none if i == drop else share(big) for i in range(6)]))
     n = lambda d: Strides(H * d, -7, d)                     # the token's stride is not used
-    return lib.mpc_linear_attention_step(ctx, q or share(big), share(big), share(big), n(dk), n(dk), n(dv), array(big), ctypes.byref(mat),
-        share(big) if state is None else state, o or share(big), so or n(dv), share(big) if out is None else out, B, H, dk, dv)
+    x = Operands(q or share(big), share(big), share(big), n(dk), n(dk), n(dv), array(big), share(big) if state is None else state, o or share(big), so or n(dv),
+                 share(big) if out is None else out)
+    return lib.mpc_linear_attention_step(ctx, ctypes.byref(x), ctypes.byref(mat), B, H, dk, dv)
 result["step"] = [step(), step(state=x, out=x), step(B=1, H=1, dk=1, dv=1), step(dk=128, dv=128),
                   step(q=none), step(state=none), step(out=none), step(o=none), step(B=0), step(dk=129), step(ws=False), step(so=Strides(0, 0, 6)), step(q=x, o=x),
                   step(state=x, o=x), step(state=x, out=shifted), step(o=x, out=x)]
@@ -198,7 +203,7 @@ old, ctx = ctx, fine
 result["frac"] = [prompt(), step()]
 ctx = old
 launches()
-result["null"] = [lib.mpc_position_bias(None, x, x, array(8), share(8), 1, 1, 1, 1, 1), lib.mpc_matvec4(None, x, array(8), array(8), share(8), 1, 1, 1, 32, 1)]
+result["null"] = [lib.mpc_linear_attention(ctx, None, ctypes.byref(Material()), 1, 1, 1, 1, 1), lib.mpc_linear_attention_step(ctx, None, ctypes.byref(StepMaterial()), 1, 1, 1, 1), lib.mpc_position_bias(None, x, x, array(8), share(8), 1, 1, 1, 1, 1), lib.mpc_matvec4(None, x, array(8), array(8), share(8), 1, 1, 1, 32, 1)]
 bias(n=0); grad(g=none); mv(K=0); prompt(T=0); step(dk=129)
 result["launched by refused calls"] = launches()
 '''
@@ -214,7 +219,7 @@ def test_refusals(tmp_path):
     assert r["matvec4 without room"] == [M, 0]
     assert r["drops"] == [E] * 10 and r["step_drops"] == [E] * 6
     assert r["step"] == [0] * 4 + [E] * 5 + [R, M] + [E] * 5
-    assert r["frac"] == [R, R] and r["null"] == [E, E] and r["launched by refused calls"] == []
+    assert r["frac"] == [R, R] and r["null"] == [E, E, E, E] and r["launched by refused calls"] == []
 
 
 def test_workspace_queries_refuse():
