@@ -530,11 +530,12 @@ int mpc_maxpool2x2_backward(mpc_ctx* ctx, mpc_cshare g, mpc_cshare s1, mpc_cshar
  * exchange.  out may be scores itself.  No workspace.
  * mpc_position_bias_grad: table_grad[u][h] = sum of g[b][h][i][j] over b and all pairs of bucket u (written, not added to);
  * scores_grad (both NULL to skip; may be g itself) = g, zero at masked pairs.  Sums mod 2^64 are exact: the result does not
- * depend on their order.
+ * depend on their order.  Workspace: the query.
  * MPC_ERANGE: n_buckets > MPC_MAX_BUCKETS, or sizes beyond 2^31. */
 #define MPC_MAX_BUCKETS 4096
 int mpc_position_bias(mpc_ctx* ctx, mpc_cshare scores, mpc_cshare table, const int32_t* buckets, mpc_share out,
                       int B, int H, int Tq, int Tk, int n_buckets);
+size_t mpc_position_bias_grad_workspace_bytes(int B, int H, int Tq, int Tk, int n_buckets);
 int mpc_position_bias_grad(mpc_ctx* ctx, mpc_cshare g, const int32_t* buckets, mpc_share table_grad, mpc_share scores_grad,
                            int B, int H, int Tq, int Tk, int n_buckets);
 

@@ -6,6 +6,8 @@
 // alone: one read).
 #include "attention.h"
 
+#include <algorithm>
+
 namespace {
 
 constexpr int kThreads = 256;
@@ -13,12 +15,17 @@ constexpr int kCols = 1024;              // columns of a tile, at most
 constexpr int kRows = 512;               // rows of a tile, at most
 constexpr int kTilePairs = 8192;         // (i, j) pairs of a tile, at most
 
+constexpr int kAtOnce = 8;               // rows of the gradient on their way at a time
+constexpr size_t kEnough = 2048;         // workgroups
+constexpr unsigned kMostWaves = 8;       // of them
+
 struct BiasArgs {
     const u64* x[2]; const u64* table[2]; const int32_t* buckets; u64* out[2];
     u64* grad[2];                        // gradient only
     unsigned BH, H, Tq, Tk; int n_buckets;
-    unsigned rows, cols, row_tiles, col_tiles;      // a tile is rows x cols
-    unsigned B, batches;                            // gradient: matrices of one head, and how many of them a workgroup sums
+    unsigned rows, cols, row_tiles, col_tiles;      // a tile is rows x cols; gradient: rows, and col_tiles of 512 diagonals
+    unsigned B, batches, splits, parts, waves;      // gradient: matrices of one head, and how many of them an item has
+    u64* partial;                                   // gradient: [party][H][bucket][part]
 };
 
 // What the distances of a tile add, and where nothing is kept: entry k is distance j - i = j0 - i0 - (rows - 1) + k.
@@ -59,54 +66,110 @@ __global__ __launch_bounds__(kThreads) void k_position_bias(BiasArgs q)
     }
 }
 
-__global__ __launch_bounds__(kThreads) void k_zero_pair(u64* a, u64* b, size_t n)
-{
-    const size_t i = (size_t)blockIdx.x * kThreads + threadIdx.x;
-    if (i < n) { a[i] = 0; b[i] = 0; }
-}
-
-// A thread walks one diagonal of the tile after another, through all rows and matrices of the workgroup, and keeps the sum in
-// a register: neighbouring threads read neighbouring words, and one sum a diagonal goes to its bucket.
+// A wave takes 128 diagonals of a block of rows, two to a lane, through all matrices of its workgroup, and keeps their sums in
+// registers: a row's words are read side by side, and one sum a diagonal goes to its bucket in LDS; the workgroups' buckets are added
+// up by a second launch (atomics on the table would need a launch ahead to clear it).  Diagonal k of a block of `rows` rows
+// from i0 on holds the pairs (i0 + r, r + k - (rows - 1)).
 template <bool SCORES>
-__global__ __launch_bounds__(kThreads) void k_position_bias_grad(BiasArgs q)
+__global__ __launch_bounds__(64 * kMostWaves) void k_position_bias_grad(BiasArgs q)
 {
     extern __shared__ u64 sums[];
-    unsigned t = blockIdx.x;
-    const unsigned jt = t % q.col_tiles; t /= q.col_tiles;
-    const unsigned it = t % q.row_tiles; t /= q.row_tiles;
-    const unsigned h = t % q.H; t /= q.H;
-    const unsigned party = t & 1, b0 = (t >> 1) * q.batches;
-    const unsigned i0 = it * q.rows, j0 = jt * q.cols;
-    const int rows = q.Tq - i0 < q.rows ? q.Tq - i0 : q.rows, cols = q.Tk - j0 < q.cols ? q.Tk - j0 : q.cols;
-    const unsigned nb = q.B - b0 < q.batches ? q.B - b0 : q.batches;
-    for (int u = threadIdx.x; u < q.n_buckets; u += kThreads) sums[u] = 0;
+    const unsigned part = blockIdx.x % q.parts, h = blockIdx.x / q.parts % q.H, party = blockIdx.x / q.parts / q.H;
+    for (int u = threadIdx.x; u < q.n_buckets; u += blockDim.x) sums[u] = 0;
     __syncthreads();
-    for (int k = threadIdx.x; k < rows + cols - 1; k += kThreads) {
-        const int u = q.buckets[(size_t)j0 + k + (q.Tq - i0 - rows)];
-        const bool kept = u >= 0 && u < q.n_buckets;
-        if (!kept && !SCORES) continue;
-        const int first = rows - 1 - k > 0 ? rows - 1 - k : 0, last = rows + cols - 1 - k < rows ? rows + cols - 1 - k : rows;   // rows of the diagonal
-        u64 sum = 0;
-        for (unsigned b = 0; b < nb; ++b) {
-            const size_t at = (((size_t)(b0 + b) * q.H + h) * q.Tq + i0) * q.Tk + j0;
-            for (int r = first; r < last; ++r) {
-                const size_t o = at + (size_t)r * q.Tk + (k + r - (rows - 1));
-                const u64 w = kept ? q.x[party][o] : 0;
-                sum += w;
-                if (SCORES) q.out[party][o] = w;
-            }
+    const unsigned items = q.row_tiles * q.col_tiles * q.splits;
+    for (unsigned item = part; item < items; item += q.parts) {
+        const unsigned dt = item % q.col_tiles, it = item / q.col_tiles % q.row_tiles, b0 = item / q.col_tiles / q.row_tiles * q.batches;
+        const unsigned i0 = it * q.rows;
+        const int rows = min(q.Tq - i0, q.rows), cols = q.Tk;
+        const unsigned nb = min(q.B - b0, q.batches);
+        const int k = (dt * blockDim.x + threadIdx.x) * 2, last = rows + cols - 2;
+        if (k <= last) {
+            const int32_t* const m = q.buckets + (q.Tq - i0 - rows);
+            const int u0 = m[k], u1 = k < last ? m[k + 1] : -1;
+            const bool kept0 = u0 >= 0 && u0 < q.n_buckets, kept1 = u1 >= 0 && u1 < q.n_buckets;
+            const int j0 = k - (rows - 1);                                 // column of the first diagonal in row 0
+            const int from = max(-j0, 0), to = min(cols - 1 - j0, rows);   // rows that have both diagonals
+            u64 s0 = 0, s1 = 0;
+            const size_t stride = (size_t)q.H * q.Tq * cols;
+            if (SCORES || kept0 || kept1)
+                for (unsigned b = 0; b < nb; ++b) {
+                    const size_t at = (b0 + b) * stride + ((size_t)h * q.Tq + i0) * cols;
+                    const u64* const x = q.x[party] + at;
+                    u64* const out = SCORES ? q.out[party] + at : nullptr;
+                    const auto one = [&](int r, int j, bool kept, u64& s) {
+                        const size_t o = (size_t)r * cols + j;
+                        const u64 w = kept ? x[o] : 0;
+                        s += w;
+                        if (SCORES) out[o] = w;
+                    };
+                    if (j0 < 0 && from - 1 < rows && k < last) one(from - 1, 0, kept1, s1);    // the row before them has the second
+                    if (to < rows && to >= 0) one(to, cols - 1, kept0, s0);                    // the row behind them the first
+                    size_t o = (size_t)from * cols + (from + j0);
+                    int r = from;
+                    for (; r + kAtOnce <= to; r += kAtOnce) {
+                        u64x2u w[kAtOnce];
+#pragma unroll
+                        for (int i = 0; i < kAtOnce; ++i) w[i] = !SCORES || kept0 || kept1 ? *reinterpret_cast<const u64x2u*>(x + o + (size_t)i * (cols + 1)) : u64x2u{ 0, 0 };
+#pragma unroll
+                        for (int i = 0; i < kAtOnce; ++i) {
+                            s0 += w[i].x; s1 += w[i].y;
+                            if (SCORES) *reinterpret_cast<u64x2u*>(out + o + (size_t)i * (cols + 1)) = u64x2u{ kept0 ? w[i].x : 0, kept1 ? w[i].y : 0 };
+                        }
+                        o += (size_t)kAtOnce * (cols + 1);
+                    }
+                    for (; r < to; ++r, o += cols + 1) {
+                        const u64x2u w = !SCORES || kept0 || kept1 ? *reinterpret_cast<const u64x2u*>(x + o) : u64x2u{ 0, 0 };
+                        s0 += w.x; s1 += w.y;
+                        if (SCORES) *reinterpret_cast<u64x2u*>(out + o) = u64x2u{ kept0 ? w.x : 0, kept1 ? w.y : 0 };
+                    }
+                }
+            if (kept0) atomicAdd((unsigned long long*)&sums[u0], (unsigned long long)s0);
+            if (kept1) atomicAdd((unsigned long long*)&sums[u1], (unsigned long long)s1);
         }
-        if (kept) atomicAdd((unsigned long long*)&sums[u], (unsigned long long)sum);
     }
     __syncthreads();
-    for (int u = threadIdx.x; u < q.n_buckets; u += kThreads)
-        if (sums[u]) atomicAdd((unsigned long long*)&q.grad[party][(size_t)u * q.H + h], (unsigned long long)sums[u]);
+    for (int u = threadIdx.x; u < q.n_buckets; u += blockDim.x)
+        q.partial[((size_t)(party * q.H + h) * q.n_buckets + u) * q.parts + part] = sums[u];
+}
+
+// the workgroups' sums of a bucket and head, a wave each
+__global__ __launch_bounds__(kThreads) void k_position_bias_sums(BiasArgs q)
+{
+    const unsigned n = 2 * q.H * (unsigned)q.n_buckets, at = blockIdx.x * (kThreads / 64) + threadIdx.x / 64, lane = threadIdx.x % 64;
+    if (at >= n) return;
+    u64 s = 0;
+    for (unsigned i = lane; i < q.parts; i += 64) s += q.partial[(size_t)at * q.parts + i];
+#pragma unroll
+    for (int d = 32; d; d /= 2) s += (u64)__shfl_xor((unsigned long long)s, d);
+    const unsigned u = at % q.n_buckets, ph = at / q.n_buckets;
+    if (lane == 0) q.grad[ph / q.H][(size_t)u * q.H + ph % q.H] = s;
+}
+
+// How the gradient is shared out: blocks of 32 rows, of fewer where that makes too few items; as many matrices to an item as leave
+// enough; and workgroups (parts) for each party and head.
+void share_out(BiasArgs& q)
+{
+    size_t one = 0;
+    for (q.rows = 32; ; q.rows /= 2) {
+        if (q.rows > q.Tq) q.rows = q.Tq;
+        const size_t diagonals = (size_t)q.rows + q.Tk - 1;
+        q.waves = (unsigned)std::min<size_t>((diagonals + 127) / 128, kMostWaves);
+        q.row_tiles = (q.Tq + q.rows - 1) / q.rows; q.col_tiles = (unsigned)((diagonals + 128 * q.waves - 1) / (128 * q.waves));
+        one = 2 * (size_t)q.H * q.row_tiles * q.col_tiles;
+        if (one * q.B >= kEnough || q.rows <= 8) break;
+    }
+    const size_t splits = std::min<size_t>((kEnough + one - 1) / one, q.B);
+    q.batches = (unsigned)((q.B + splits - 1) / splits);
+    q.splits = (q.B + q.batches - 1) / q.batches;
+    const size_t items = (size_t)q.row_tiles * q.col_tiles * q.splits;
+    q.parts = (unsigned)std::min<size_t>(items, (kEnough + 2 * q.H - 1) / (2 * q.H));
 }
 
 int bias_shape(BiasArgs& q, int B, int H, int Tq, int Tk, int n_buckets)
 {
     if (B <= 0 || H <= 0 || Tq <= 0 || Tk <= 0 || n_buckets <= 0) return MPC_EINVAL;
-    if (n_buckets > MPC_MAX_BUCKETS || (long long)Tq + Tk - 1 > INT32_MAX || (long long)B * H > INT32_MAX) return MPC_ERANGE;
+    if (n_buckets > MPC_MAX_BUCKETS || (long long)Tq + Tk - 1 > INT32_MAX || (long long)B * H > INT32_MAX || 2ll * H * n_buckets > INT32_MAX) return MPC_ERANGE;
     q.B = B; q.H = H; q.BH = (unsigned)B * H; q.Tq = Tq; q.Tk = Tk; q.n_buckets = n_buckets;
     return MPC_OK;
 }
@@ -114,6 +177,14 @@ int bias_shape(BiasArgs& q, int B, int H, int Tq, int Tk, int n_buckets)
 }  // namespace
 
 extern "C" {
+
+size_t mpc_position_bias_grad_workspace_bytes(int B, int H, int Tq, int Tk, int n_buckets)
+{
+    BiasArgs q{};
+    if (bias_shape(q, B, H, Tq, Tk, n_buckets) != MPC_OK) return 0;
+    share_out(q);
+    return align_up(2 * (size_t)H * n_buckets * q.parts * 8);
+}
 
 int mpc_position_bias(mpc_ctx* c, mpc_cshare x, mpc_cshare table, const int32_t* buckets, mpc_share out,
                       int B, int H, int Tq, int Tk, int n_buckets)
@@ -149,22 +220,19 @@ int mpc_position_bias_grad(mpc_ctx* c, mpc_cshare g, const int32_t* buckets, mpc
     if (!outputs_apart(table_grad, table_bytes, g, bytes, false)) return MPC_EINVAL;
     if (scores && (!outputs_apart(scores_grad, bytes, g, bytes, true) ||
                    !outputs_apart(table_grad, table_bytes, mpc_cshare{ { scores_grad.p[0], scores_grad.p[1] } }, bytes, false))) return MPC_EINVAL;
-    q.cols = Tk < kCols ? Tk : kCols;
-    q.rows = Tq < 32 ? Tq : 32;
-    q.row_tiles = (q.Tq + q.rows - 1) / q.rows; q.col_tiles = (q.Tk + q.cols - 1) / q.cols;
-    const size_t one = 2 * (size_t)H * q.row_tiles * q.col_tiles;
-    size_t splits = (2048 + one - 1) / one; if (splits > q.B) splits = q.B;
-    q.batches = (unsigned)((q.B + splits - 1) / splits);
-    const size_t grid = one * ((q.B + q.batches - 1) / q.batches);
-    if (grid > INT32_MAX) return MPC_ERANGE;
+    share_out(q);
+    if ((size_t)q.row_tiles * q.col_tiles * q.splits > INT32_MAX || 2 * (size_t)H * q.parts > INT32_MAX) return MPC_ERANGE;
+    WsAlloc ws(c->ws, c->ws_bytes);
+    q.partial = ws.take<u64>(2 * (size_t)H * n_buckets * q.parts);
+    if (!ws.ok) return MPC_ENOMEM;
     for (int i = 0; i < 2; ++i) { q.x[i] = g.p[i]; q.grad[i] = table_grad.p[i]; q.out[i] = scores_grad.p[i]; }
     q.buckets = buckets;
     MPC_TRY(lane_first(c));
-    const size_t words = (size_t)n_buckets * H;
-    k_zero_pair<<<dim3((unsigned)((words + kThreads - 1) / kThreads)), kThreads, 0, c->s[0]>>>(table_grad.p[0], table_grad.p[1], words);
+    const dim3 grid(2 * (unsigned)H * q.parts), block(64 * q.waves);
     const size_t lds = (size_t)n_buckets * 8;
-    if (scores) k_position_bias_grad<true><<<dim3((unsigned)grid), kThreads, lds, c->s[0]>>>(q);
-    else k_position_bias_grad<false><<<dim3((unsigned)grid), kThreads, lds, c->s[0]>>>(q);
+    if (scores) k_position_bias_grad<true><<<grid, block, lds, c->s[0]>>>(q);
+    else k_position_bias_grad<false><<<grid, block, lds, c->s[0]>>>(q);
+    k_position_bias_sums<<<dim3((unsigned)((2 * (size_t)H * n_buckets + 3) / 4)), kThreads, 0, c->s[0]>>>(q);
     MPC_HIP(c, hipGetLastError());
     return lane_fanout(c);
 }

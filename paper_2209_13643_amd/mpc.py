@@ -81,7 +81,7 @@ EXPORTS = [
     "mpc_conv2d3_grad_x_workspace_bytes", "mpc_conv2d3_grad_w_workspace_bytes", "mpc_conv2d3_grad_x", "mpc_conv2d3_grad_w",
     "mpc_add3", "mpc_sub3", "mpc_mul3_workspace_bytes", "mpc_mul3", "mpc_relu3_backward", "mpc_maxpool3_signs",
     "mpc_maxpool3_backward_workspace_bytes", "mpc_maxpool3_backward",
-    "mpc_position_bias", "mpc_position_bias_grad", "mpc_matvec4", "mpc_matvec4_workspace_bytes", "mpc_linear_attention_workspace_bytes", "mpc_linear_attention",
+    "mpc_position_bias", "mpc_position_bias_grad", "mpc_position_bias_grad_workspace_bytes", "mpc_matvec4", "mpc_matvec4_workspace_bytes", "mpc_linear_attention_workspace_bytes", "mpc_linear_attention",
     "mpc_linear_attention_step_workspace_bytes", "mpc_linear_attention_step",
 ]
 
@@ -204,6 +204,7 @@ def lib():
     L.mpc_maxpool3_backward_workspace_bytes.argtypes = [c_int] * 4; L.mpc_maxpool3_backward_workspace_bytes.restype = c_size_t
     L.mpc_maxpool3_backward.argtypes = [c_void_p] + [CShare3] * 10 + [c_int] * 4
     L.mpc_position_bias.argtypes = [c_void_p, CShare, CShare, c_void_p, CShare] + [c_int] * 5
+    L.mpc_position_bias_grad_workspace_bytes.argtypes = [c_int] * 5; L.mpc_position_bias_grad_workspace_bytes.restype = c_size_t
     L.mpc_position_bias_grad.argtypes = [c_void_p, CShare, c_void_p, CShare, CShare] + [c_int] * 5
     L.mpc_matvec4_workspace_bytes.argtypes = [c_int] * 3; L.mpc_matvec4_workspace_bytes.restype = c_size_t
     L.mpc_matvec4.argtypes = [c_void_p, CShare, c_void_p, c_void_p, CShare] + [c_int] * 5
@@ -1007,8 +1008,12 @@ class Lane:
         s, o = _dense_share(g, shape, at, "g"), _dense_share(out, (n_buckets, H), at, "out")
         so = _dense_share(scores_out, shape, at, "scores_out") if scores_out is not None else CShare()
         m = _dense(buckets, (Tq + Tk - 1,), torch.int32, at, "buckets")
+        L = lib()
+        need = L.mpc_position_bias_grad_workspace_bytes(B, H, Tq, Tk, n_buckets)
+        if need == 0 or need > self._ws_bytes:
+            self.reserve(need)
         self._pending += (*g, buckets, *out, *(scores_out or ()))
-        self._check(lib().mpc_position_bias_grad(self._h, s, m, o, so, B, H, Tq, Tk, n_buckets))
+        self._check(L.mpc_position_bias_grad(self._h, s, m, o, so, B, H, Tq, Tk, n_buckets))
         return out, scores_out
 
     def matvec4(self, x, w, scales, group, scale_bits=16, out=None):

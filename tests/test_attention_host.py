@@ -144,7 +144,7 @@ for n in ("mpc_linear_attention_workspace_bytes", "mpc_linear_attention_step_wor
 P = c_void_p
 lib.mpc_position_bias.argtypes = [P, Share, Share, P, Share] + [c_int] * 5
 lib.mpc_position_bias_grad.argtypes = [P, Share, P, Share, Share] + [c_int] * 5
-lib.mpc_matvec4_workspace_bytes.restype = c_size_t
+lib.mpc_matvec4_workspace_bytes.restype = lib.mpc_position_bias_grad_workspace_bytes.restype = c_size_t
 lib.mpc_matvec4.argtypes = [P, Share, P, P, Share] + [c_int] * 5
 lib.mpc_linear_attention.argtypes = [P, P, P] + [c_int] * 5
 lib.mpc_linear_attention_step.argtypes = [P, P, P] + [c_int] * 4
@@ -162,6 +162,7 @@ result["bias"] = [bias(), bias(x=x, o=x), bias(x=none), bias(t=half), bias(o=non
                   bias(n=4097), bias(Tq=1 << 30, Tk=(1 << 30) + 2), bias(x=x, o=shifted), bias(x=x, o=crossed), bias(x=x, o=same), bias(t=x, o=x)]
 def grad(g=None, m=None, t=None, s=None, B=2, H=3, Tq=8, Tk=8, n=4):
     return lib.mpc_position_bias_grad(ctx, g or share(big), array(big) if m is None else m or None, t or share(big), s or none, B, H, Tq, Tk, n)
+lib.mpc_ctx_set_workspace(ctx, array(big), big)
 result["grad"] = [grad(), grad(g=x, s=x), grad(g=none), grad(t=none), grad(s=half), grad(m=0), grad(B=0), grad(n=5000), grad(g=x, s=shifted), grad(g=x, t=x), grad(s=x, t=x)]
 def mv(x=None, w=None, s=None, z=None, M=2, K=100, N=5, group=32, bits=16):
     return lib.mpc_matvec4(ctx, x or share(big), array(big) if w is None else w or None, array(big) if s is None else s or None, z or share(big), M, K, N, group, bits)
@@ -182,6 +183,11 @@ result["prompt"] = [prompt(), prompt(state=none), prompt(out=none), prompt(state
                     prompt(dv=0), prompt(dk=129), prompt(dv=200), prompt(ws=False), prompt(sq=Strides(-1, 8, 8)), prompt(so=Strides(0, 18, 6)), prompt(so=Strides(1260, 18, 5)),
                     prompt(so=Strides(1259, 18, 6)), prompt(q=x, o=x), prompt(q=x, out=x), prompt(state=x, o=x), prompt(o=x, out=x), prompt(state=x, out=shifted),
                     prompt(B=1 << 20, H=1 << 12)]
+need = lib.mpc_position_bias_grad_workspace_bytes(2, 3, 8, 8, 4)
+lib.mpc_ctx_set_workspace(ctx, array(need), need - 1)
+result["grad without room"] = grad()
+lib.mpc_ctx_set_workspace(ctx, array(need), need)
+result["grad with room"] = grad()
 lib.mpc_ctx_set_workspace(ctx, array(4096), 4096)
 result["matvec4 without room"] = [mv(M=16, K=4096, N=4096), mv(M=16, K=4096, N=100)]
 result["drops"] = [prompt(drop=i) for i in range(10)]
@@ -216,6 +222,7 @@ def test_refusals(tmp_path):
     assert r["grad"] == [0, 0] + [E] * 5 + [R] + [E] * 3
     assert r["matvec4"] == [0] * 6 + [E] * 15 + [R, R] + [E] * 3
     assert r["prompt"] == [0] * 7 + [E] * 11 + [R, R, M] + [E] * 9 + [R]
+    assert r["grad without room"] == M and r["grad with room"] == 0
     assert r["matvec4 without room"] == [M, 0]
     assert r["drops"] == [E] * 10 and r["step_drops"] == [E] * 6
     assert r["step"] == [0] * 4 + [E] * 5 + [R, M] + [E] * 5
