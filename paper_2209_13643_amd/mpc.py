@@ -8,6 +8,7 @@ library is missing or the device is absent, calls raise.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 import struct
 import threading
@@ -308,53 +309,46 @@ def _material3(mat: dict, n: int, packed: bool = False) -> Relu3Material:
 # call names 24 tensors.
 _pack_operands = struct.Struct("6Q9qQ4Q3q2Q").pack
 _pack_prompt, _pack_step = struct.Struct("20Q").pack, struct.Struct("12Q").pack
-_int64 = torch.int64
+
+
+# One question for all tensors of a call at a time: mapping the methods is twice as fast as asking tensor by tensor.
+_size, _stride, _numel, _contiguous, _device, _ptr = (torch.Tensor.size, torch.Tensor.stride, torch.Tensor.numel, torch.Tensor.is_contiguous,
+                                                      torch.Tensor.get_device, torch.Tensor.data_ptr)
+_dtype = operator.attrgetter("dtype")
+_only_int64 = {torch.int64}
+
+
+def _refuse(names, tensors, wanted, index, what):
+    got = "; ".join(f"'{n}': {t.dtype} {list(t.shape)} strides {list(t.stride())} on {t.device}, expected {list(w)}" for n, t, w in zip(names, tensors, wanted))
+    raise ValueError(f"{what} on device {index} expected: {got}")
 
 
 def _dense(t, shape, dtype, index, name):
-    """Checked device address of a dense tensor on device `index`."""
+    """Checked device address of a dense tensor."""
     if t.dtype is not dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous():
-        raise ValueError(f"'{name}': contiguous {dtype} tensor of shape {list(shape)} on device {index} expected, "
-                         f"got {t.dtype} {list(t.shape)} on {t.device}")
+        _refuse([name], [t], [shape], index, f"a contiguous {dtype} tensor")
     return t.data_ptr()
 
 
-def _two(pair, name):
-    if len(pair) != 2:
-        raise ValueError(f"'{name}': a sharing is a pair of tensors")
-    return pair
-
-
-def _dense_share(pair, shape, index, name):
-    a, b = _two(pair, name)
-    return CShare.from_buffer_copy(_pack2(_dense(a, shape, _int64, index, name), _dense(b, shape, _int64, index, name)))
-
-
-def _heads(pair, shape, index, name):
-    """(addresses, strides) of a sharing of [B, (T,) H, d]; the last axis is dense, the others lie as they lie."""
-    a, b = _two(pair, name)
-    st = a.stride()
-    if (a.dtype is not _int64 or b.dtype is not _int64 or a.shape != shape or b.shape != shape or a.get_device() != index
-            or b.get_device() != index or b.stride() != st or (st[-1] != 1 and shape[-1] != 1)):
-        raise ValueError(f"'{name}': int64 tensors of shape {list(shape)} on device {index}, dense in the last axis and with the same "
-                         f"strides for both shares expected, got {[(t.dtype, list(t.shape), t.stride(), str(t.device)) for t in pair]}")
-    return (a.data_ptr(), b.data_ptr()), (st[:3] if len(st) == 4 else (st[0], 0, st[1]))
-
-
-def _attention_material(names, mat, words, index, keep):
-    """Addresses of a material's dense arrays, by the number of their words; the tensors are added to `keep`."""
+def _pairs(*sharings):
     out = []
-    for n in names:
-        if n not in mat:
-            raise ValueError(f"material lacks '{n}'")
-        pair, want = _two(mat[n], n), words[n]
-        for t in pair:
-            if t.numel() != want or t.dtype is not _int64 or t.get_device() != index or not t.is_contiguous():
-                raise ValueError(f"material '{n}': {want} dense int64 words per party on device {index} expected, "
-                                 f"got {t.dtype} {list(t.shape)} on {t.device}")
-            out.append(t.data_ptr())
-        keep += pair
+    for name, s in sharings:
+        if len(s) != 2:
+            raise ValueError(f"'{name}': a sharing is a pair of tensors")
+        out += s
     return out
+
+
+def _words(tensors, shapes, index, names):
+    """Checked device addresses of dense int64 tensors of the given shapes."""
+    if (list(map(_size, tensors)) != shapes or set(map(_dtype, tensors)) != _only_int64 or set(map(_device, tensors)) != {index}
+            or not all(map(_contiguous, tensors))):
+        _refuse([n for n in names for _ in range(2)], tensors, shapes, index, "contiguous int64 tensors")
+    return list(map(_ptr, tensors))
+
+
+def _share_at(addresses, i):
+    return CShare.from_buffer_copy(_pack2(addresses[i], addresses[i + 1]))
 
 
 def to_device(arr, device="cuda:0"):
@@ -988,52 +982,58 @@ class Lane:
     def position_bias(self, scores, table, buckets, out=None):
         """scores [B, H, Tq, Tk] + table [n, H] at the public bucket of every pair: buckets int32 [Tq + Tk - 1], entry
         j - i + Tq - 1 of query i and key j; an entry outside [0, n) masks its pairs (zero).  out may be scores."""
-        shape, at = scores[0].shape, self._index
+        shape = scores[0].shape
         B, H, Tq, Tk = shape
         n = table[0].shape[0]
         out = out if out is not None else (torch.empty_like(scores[0]), torch.empty_like(scores[1]))
-        s, t, o = _dense_share(scores, shape, at, "scores"), _dense_share(table, (n, H), at, "table"), _dense_share(out, shape, at, "out")
-        m = _dense(buckets, (Tq + Tk - 1,), torch.int32, at, "buckets")
-        self._pending += (*scores, *table, buckets, *out)
-        self._check(lib().mpc_position_bias(self._h, s, t, m, o, B, H, Tq, Tk, n))
+        ts, small = _pairs(("scores", scores), ("table", table), ("out", out)), (n, H)
+        at = _words(ts, [shape, shape, small, small, shape, shape], self._index, ("scores", "table", "out"))
+        m = _dense(buckets, (Tq + Tk - 1,), torch.int32, self._index, "buckets")
+        ts.append(buckets)
+        self._pending += ts
+        self._check(lib().mpc_position_bias(self._h, _share_at(at, 0), _share_at(at, 2), m, _share_at(at, 4), B, H, Tq, Tk, n))
         return out
 
     def position_bias_grad(self, g, buckets, n_buckets, out=None, scores_out=None):
         """Gradient of position_bias for its output's g: (table's [n_buckets, H], scores').  The scores' gradient is g with
         zeros at masked pairs; it is written to scores_out (may be g), or not at all if that is None."""
-        shape, at = g[0].shape, self._index
+        shape = g[0].shape
         B, H, Tq, Tk = shape
         if out is None:
-            out = tuple(torch.empty((n_buckets, H), dtype=_int64, device=self.device) for _ in range(2))
-        s, o = _dense_share(g, shape, at, "g"), _dense_share(out, (n_buckets, H), at, "out")
-        so = _dense_share(scores_out, shape, at, "scores_out") if scores_out is not None else CShare()
-        m = _dense(buckets, (Tq + Tk - 1,), torch.int32, at, "buckets")
+            out = tuple(torch.empty((n_buckets, H), dtype=torch.int64, device=self.device) for _ in range(2))
+        ts, small = _pairs(("g", g), ("out", out), ("scores_out", scores_out if scores_out is not None else g)), (n_buckets, H)
+        at = _words(ts, [shape, shape, small, small, shape, shape], self._index, ("g", "out", "scores_out"))
+        m = _dense(buckets, (Tq + Tk - 1,), torch.int32, self._index, "buckets")
         L = lib()
         need = L.mpc_position_bias_grad_workspace_bytes(B, H, Tq, Tk, n_buckets)
         if need == 0 or need > self._ws_bytes:
             self.reserve(need)
-        self._pending += (*g, buckets, *out, *(scores_out or ()))
-        self._check(L.mpc_position_bias_grad(self._h, s, m, o, so, B, H, Tq, Tk, n_buckets))
+        ts.append(buckets)
+        self._pending += ts
+        self._check(L.mpc_position_bias_grad(self._h, _share_at(at, 0), m, _share_at(at, 2), _share_at(at, 4) if scores_out is not None else CShare(),
+                                             B, H, Tq, Tk, n_buckets))
         return out, scores_out
 
     def matvec4(self, x, w, scales, group, scale_bits=16, out=None):
         """x [M, K] times public 4-bit weights: w uint8 [N, 16 ceil(K / 32)] (attention.pack_weights4), scales int32
         [N, ceil(K / group)] with scale_bits fraction bits.  z [M, N] in x's fixed point."""
-        shape, at = x[0].shape, self._index
+        shape = x[0].shape
         M, K = shape
         N = w.shape[0]
-        out = out if out is not None else tuple(torch.empty((M, N), dtype=_int64, device=self.device) for _ in range(2))
+        out = out if out is not None else tuple(torch.empty((M, N), dtype=torch.int64, device=self.device) for _ in range(2))
         if group <= 0:
             raise ValueError(f"group: a positive number of columns expected, got {group}")
-        xs, zs = _dense_share(x, shape, at, "x"), _dense_share(out, (M, N), at, "out")
-        wp = _dense(w, (N, (K + 31) // 32 * 16), torch.uint8, at, "w")
-        sp = _dense(scales, (N, -(-K // group)), torch.int32, at, "scales")
+        ts, result = _pairs(("x", x), ("out", out)), (M, N)
+        at = _words(ts, [shape, shape, result, result], self._index, ("x", "out"))
+        wp = _dense(w, (N, (K + 31) // 32 * 16), torch.uint8, self._index, "w")
+        sp = _dense(scales, (N, -(-K // group)), torch.int32, self._index, "scales")
         L = lib()
         need = L.mpc_matvec4_workspace_bytes(M, K, N)
         if need > self._ws_bytes:
             self.reserve(need)
-        self._pending += (*x, w, scales, *out)
-        self._check(L.mpc_matvec4(self._h, xs, wp, sp, zs, M, K, N, group, scale_bits))
+        ts += (w, scales)
+        self._pending += ts
+        self._check(L.mpc_matvec4(self._h, _share_at(at, 0), wp, sp, _share_at(at, 2), M, K, N, group, scale_bits))
         return out
 
     def linear_attention(self, q, k, v, decay, mat, state=None, out=None, state_out=None):
@@ -1044,9 +1044,8 @@ class Lane:
         B, T, H, dk = q[0].shape
         dv, nc = v[0].shape[-1], -(-T // ATTENTION_CHUNK)
         rows, tok, cells = B * H * T, B * H * T * ATTENTION_CHUNK, B * H * nc * dk * dv
-        words = dict(a_q=rows * dk, a_k=rows * dk, a_qd=rows * dk, a_kd=rows * dk, a_v=rows * dv, a_w=tok, a_s=cells, c_p=tok, c_u=cells,
-                     c_o=rows * dv)
-        return self._attend(q, k, v, decay, mat, state, out, state_out, (B, T, H), dk, dv, words)
+        words = (rows * dk, rows * dk, rows * dk, rows * dk, rows * dv, tok, cells, tok, cells, rows * dv)
+        return self._attend(q, k, v, decay, mat, state, out, state_out, (B, T, H), dk, dv, _ATTENTION_MASKS, words)
 
     def linear_attention_step(self, q, k, v, decay, mat, state, out=None, state_out=None):
         """One token of linear_attention: q, k [B, H, dk], v [B, H, dv], state [B, H, dk, dv]; mat as
@@ -1055,28 +1054,47 @@ class Lane:
         dv, n = v[0].shape[-1], B * H
         if state is None:
             raise ValueError("a step goes on from a state")
-        words = dict(a_q=n * dk, a_k=n * dk, a_v=n * dv, a_s=n * dk * dv, c_u=n * dk * dv, c_o=n * dv)
-        return self._attend(q, k, v, decay, mat, state, out, state_out, (B, H), dk, dv, words)
+        words = (n * dk, n * dk, n * dv, n * dk * dv, n * dk * dv, n * dv)
+        return self._attend(q, k, v, decay, mat, state, out, state_out, (B, H), dk, dv, _STEP_MASKS, words)
 
-    def _attend(self, q, k, v, decay, mat, state, out, state_out, lead, dk, dv, words):
-        B, H, at, L, prompt = lead[0], lead[-1], self._index, lib(), len(lead) == 3
+    def _attend(self, q, k, v, decay, mat, state, out, state_out, lead, dk, dv, masks, words):
+        B, H, index, L, prompt = lead[0], lead[-1], self._index, lib(), len(lead) == 3
         cell = (B, H, dk, dv)
-        out = out if out is not None else tuple(torch.empty((*lead, dv), dtype=_int64, device=self.device) for _ in range(2))
-        state_out = state_out if state_out is not None else tuple(torch.empty(cell, dtype=_int64, device=self.device) for _ in range(2))
-        (qs, sq), (ks, sk) = _heads(q, (*lead, dk), at, "q"), _heads(k, (*lead, dk), at, "k")
-        (vs, sv), (os_, so) = _heads(v, (*lead, dv), at, "v"), _heads(out, (*lead, dv), at, "out")
-        st = [_dense(t, cell, _int64, at, "state") for t in _two(state, "state")] if state is not None else (0, 0)
-        sn = [_dense(t, cell, _int64, at, "state_out") for t in _two(state_out, "state_out")]
-        d = _dense(decay, (H, ATTENTION_CHUNK + 1), torch.int32, at, "decay")
-        keep = [*q, *k, *v, decay, *out, *state_out, *(state or ())]
-        m = _attention_material(_ATTENTION_MASKS if prompt else _STEP_MASKS, mat, words, at, keep)
+        out = out if out is not None else tuple(torch.empty((*lead, dv), dtype=torch.int64, device=self.device) for _ in range(2))
+        state_out = state_out if state_out is not None else tuple(torch.empty(cell, dtype=torch.int64, device=self.device) for _ in range(2))
+        # q, k, v and the output lie as they lie, dense in the last axis; both shares alike
+        ts = _pairs(("q", q), ("k", k), ("v", v), ("out", out))
+        row, col = (*lead, dk), (*lead, dv)
+        strides = list(map(_stride, ts))
+        if (list(map(_size, ts)) != [row, row, row, row, col, col, col, col] or set(map(_dtype, ts)) != _only_int64
+                or set(map(_device, ts)) != {index} or strides[0::2] != strides[1::2]
+                or any(st[-1] != 1 for st in strides[:4] if dk > 1) or any(st[-1] != 1 for st in strides[4:] if dv > 1)):
+            _refuse([n for n in ("q", "k", "v", "out") for _ in range(2)], ts, [row] * 4 + [col] * 4, index,
+                    "int64 tensors, dense in the last axis and with the same strides for both shares,")
+        at = list(map(_ptr, ts))
+        dense = _pairs(("state", state), ("state_out", state_out)) if state is not None else _pairs(("state_out", state_out))
+        st = _words(dense, [cell] * len(dense), index, ("state", "state_out")[-len(dense) // 2:])
+        if state is None:
+            st = [0, 0, *st]
+        try:
+            ms = _pairs(*[(n, mat[n]) for n in masks])
+        except KeyError as e:
+            raise ValueError(f"material lacks {e}") from None
+        if (list(map(_numel, ms))[0::2] != list(words) or list(map(_numel, ms))[1::2] != list(words) or set(map(_dtype, ms)) != _only_int64
+                or set(map(_device, ms)) != {index} or not all(map(_contiguous, ms))):
+            _refuse([n for n in masks for _ in range(2)], ms, [(n,) for n in words for _ in range(2)], index, "dense int64 material of these numbers of words")
+        d = _dense(decay, (H, ATTENTION_CHUNK + 1), torch.int32, index, "decay")
         need = (L.mpc_linear_attention_workspace_bytes if prompt else L.mpc_linear_attention_step_workspace_bytes)(*lead, dk, dv)
         if need == 0 or need > self._ws_bytes:
             self.reserve(need)
-        self._pending += keep
-        x = _pack_operands(*qs, *ks, *vs, *sq, *sk, *sv, d, *st, *os_, *so, *sn)
-        self._check(L.mpc_linear_attention(self._h, x, _pack_prompt(*m), *lead, dk, dv) if prompt else
-                    L.mpc_linear_attention_step(self._h, x, _pack_step(*m), *lead, dk, dv))
+        self._pending += ts
+        self._pending += dense
+        self._pending += ms
+        self._pending.append(decay)
+        sq, sk, sv, so = (s[:3] if prompt else (s[0], 0, s[1]) for s in strides[0::2])
+        x = _pack_operands(*at[:6], *sq, *sk, *sv, d, st[0], st[1], at[6], at[7], *so, st[2], st[3])
+        self._check(L.mpc_linear_attention(self._h, x, _pack_prompt(*map(_ptr, ms)), *lead, dk, dv) if prompt else
+                    L.mpc_linear_attention_step(self._h, x, _pack_step(*map(_ptr, ms)), *lead, dk, dv))
         return out, state_out
 
     def ring_matmul(self, L, R):
