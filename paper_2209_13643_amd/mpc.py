@@ -1044,7 +1044,7 @@ class Lane:
         B, T, H, dk = q[0].shape
         dv, nc = v[0].shape[-1], -(-T // ATTENTION_CHUNK)
         rows, tok, cells = B * H * T, B * H * T * ATTENTION_CHUNK, B * H * nc * dk * dv
-        words = (rows * dk, rows * dk, rows * dk, rows * dk, rows * dv, tok, cells, tok, cells, rows * dv)
+        words = [rows * dk, rows * dk, rows * dk, rows * dk, rows * dv, tok, cells, tok, cells, rows * dv]
         return self._attend(q, k, v, decay, mat, state, out, state_out, (B, T, H), dk, dv, _ATTENTION_MASKS, words)
 
     def linear_attention_step(self, q, k, v, decay, mat, state, out=None, state_out=None):
@@ -1054,7 +1054,7 @@ class Lane:
         dv, n = v[0].shape[-1], B * H
         if state is None:
             raise ValueError("a step goes on from a state")
-        words = (n * dk, n * dk, n * dv, n * dk * dv, n * dk * dv, n * dv)
+        words = [n * dk, n * dk, n * dv, n * dk * dv, n * dk * dv, n * dv]
         return self._attend(q, k, v, decay, mat, state, out, state_out, (B, H), dk, dv, _STEP_MASKS, words)
 
     def _attend(self, q, k, v, decay, mat, state, out, state_out, lead, dk, dv, masks, words):
@@ -1062,39 +1062,41 @@ class Lane:
         cell = (B, H, dk, dv)
         out = out if out is not None else tuple(torch.empty((*lead, dv), dtype=torch.int64, device=self.device) for _ in range(2))
         state_out = state_out if state_out is not None else tuple(torch.empty(cell, dtype=torch.int64, device=self.device) for _ in range(2))
-        # q, k, v and the output lie as they lie, dense in the last axis; both shares alike
-        ts = _pairs(("q", q), ("k", k), ("v", v), ("out", out))
         row, col = (*lead, dk), (*lead, dv)
-        strides = list(map(_stride, ts))
-        if (list(map(_size, ts)) != [row, row, row, row, col, col, col, col] or set(map(_dtype, ts)) != _only_int64
-                or set(map(_device, ts)) != {index} or strides[0::2] != strides[1::2]
-                or any(st[-1] != 1 for st in strides[:4] if dk > 1) or any(st[-1] != 1 for st in strides[4:] if dv > 1)):
-            _refuse([n for n in ("q", "k", "v", "out") for _ in range(2)], ts, [row] * 4 + [col] * 4, index,
-                    "int64 tensors, dense in the last axis and with the same strides for both shares,")
-        at = list(map(_ptr, ts))
-        dense = _pairs(("state", state), ("state_out", state_out)) if state is not None else _pairs(("state_out", state_out))
-        st = _words(dense, [cell] * len(dense), index, ("state", "state_out")[-len(dense) // 2:])
-        if state is None:
-            st = [0, 0, *st]
+        # q, k, v and the output lie as they lie, dense in the last axis and both shares alike; all else is dense
         try:
-            ms = _pairs(*[(n, mat[n]) for n in masks])
+            (q0, q1), (k0, k1), (v0, v1), (o0, o1), (n0, n1) = q, k, v, out, state_out
+            ts = [q0, q1, k0, k1, v0, v1, o0, o1, n0, n1]
+            if state is not None:
+                s0, s1 = state
+                ts += (s0, s1)
+            n_x = len(ts)
+            for name in masks:
+                m0, m1 = mat[name]
+                ts += (m0, m1)
         except KeyError as e:
             raise ValueError(f"material lacks {e}") from None
-        if (list(map(_numel, ms))[0::2] != list(words) or list(map(_numel, ms))[1::2] != list(words) or set(map(_dtype, ms)) != _only_int64
-                or set(map(_device, ms)) != {index} or not all(map(_contiguous, ms))):
-            _refuse([n for n in masks for _ in range(2)], ms, [(n,) for n in words for _ in range(2)], index, "dense int64 material of these numbers of words")
+        shapes = [row, row, row, row, col, col, col, col, cell, cell, cell, cell][:n_x]
+        numbers = list(map(_numel, ts[n_x:]))
+        strides = list(map(_stride, ts[:8]))
+        if (set(map(_dtype, ts)) != _only_int64 or set(map(_device, ts)) != {index} or list(map(_size, ts[:n_x])) != shapes
+                or not all(map(_contiguous, ts[8:])) or numbers[0::2] != words or numbers[1::2] != words or strides[0::2] != strides[1::2]
+                or (dk > 1 and (strides[0][-1] != 1 or strides[2][-1] != 1)) or (dv > 1 and (strides[4][-1] != 1 or strides[6][-1] != 1))):
+            names = [n for n in ("q", "k", "v", "out", "state_out", "state")[:n_x // 2] + masks for _ in range(2)]
+            _refuse(names, ts, shapes + [(n,) for n in words for _ in range(2)], index, "int64 tensors, q, k, v and the output dense in the last axis "
+                    "and with the same strides for both shares, the others dense, the material by its number of words,")
+        at = list(map(_ptr, ts))
         d = _dense(decay, (H, ATTENTION_CHUNK + 1), torch.int32, index, "decay")
         need = (L.mpc_linear_attention_workspace_bytes if prompt else L.mpc_linear_attention_step_workspace_bytes)(*lead, dk, dv)
         if need == 0 or need > self._ws_bytes:
             self.reserve(need)
+        ts.append(decay)
         self._pending += ts
-        self._pending += dense
-        self._pending += ms
-        self._pending.append(decay)
-        sq, sk, sv, so = (s[:3] if prompt else (s[0], 0, s[1]) for s in strides[0::2])
-        x = _pack_operands(*at[:6], *sq, *sk, *sv, d, st[0], st[1], at[6], at[7], *so, st[2], st[3])
-        self._check(L.mpc_linear_attention(self._h, x, _pack_prompt(*map(_ptr, ms)), *lead, dk, dv) if prompt else
-                    L.mpc_linear_attention_step(self._h, x, _pack_step(*map(_ptr, ms)), *lead, dk, dv))
+        sq, sk, sv, so = strides[0::2]
+        sq, sk, sv, so = (sq[:3], sk[:3], sv[:3], so[:3]) if prompt else ((sq[0], 0, sq[1]), (sk[0], 0, sk[1]), (sv[0], 0, sv[1]), (so[0], 0, so[1]))
+        x = _pack_operands(*at[:6], *sq, *sk, *sv, d, *(at[10:12] if state is not None else (0, 0)), at[6], at[7], *so, at[8], at[9])
+        self._check(L.mpc_linear_attention(self._h, x, _pack_prompt(*at[n_x:]), *lead, dk, dv) if prompt else
+                    L.mpc_linear_attention_step(self._h, x, _pack_step(*at[n_x:]), *lead, dk, dv))
         return out, state_out
 
     def ring_matmul(self, L, R):
