@@ -140,6 +140,28 @@ def test_position_bias_large(mpc, lane, attention):
             assert torch.equal(grad[p], want)
 
 
+def test_position_bias_beyond_32_bit_offsets(mpc, lane, attention):
+    """Shares of more than 2^32 bytes each, compared at the ends and across the border; the gradient as sums of int64 tensors."""
+    B, H, T, n = 2, 48, 2400, 8
+    g = torch.Generator(device="cuda:0").manual_seed(2)
+    x = tuple(torch.randint(-2 ** 63, 2 ** 63 - 1, (B, H, T, T), generator=g, device="cuda:0") for _ in range(2))
+    t = tuple(torch.randint(-2 ** 63, 2 ** 63 - 1, (n, H), generator=g, device="cuda:0") for _ in range(2))
+    assert x[0].numel() * 8 > 2 ** 32
+    m = attention.relative_buckets(T, T, n, 40, True).cuda()
+    torch.cuda.synchronize()
+    y = lane.position_bias(x, t, m)
+    grad, _ = lane.position_bias_grad(x, m, n)
+    lane.sync()
+    at = m.long()[torch.arange(T, device="cuda:0") - torch.arange(T, device="cuda:0")[:, None] + T - 1]
+    kept = at >= 0
+    for p in range(2):
+        for b, h in ((0, 0), (1, 44), (1, 45), (1, 46), (1, 47)):
+            assert torch.equal(y[p][b, h], (x[p][b, h] + t[p][at.clamp(min=0), h]) * kept)
+            want = torch.zeros(n, dtype=torch.int64, device="cuda:0")
+            want.index_add_(0, at.clamp(min=0).flatten(), ((x[p][0, h] + x[p][1, h]) * kept).flatten())
+            assert torch.equal(grad[p][:, h], want)
+
+
 # ------------------------------------------------------------------------------------------------ 4-bit weights
 @pytest.mark.parametrize("M,K,N,group", [(1, 1, 1, 32), (1, 32, 16, 32), (2, 33, 5, 32), (1, 64, 17, 64), (3, 100, 40, 64), (1, 127, 15, 128), (4, 129, 33, 128),
                                          (1, 700, 64, 128), (5, 1000, 50, 32), (8, 513, 31, 64), (9, 300, 20, 256), (17, 96, 70, 32), (1, 2500, 130, 32),
@@ -332,6 +354,52 @@ def test_other_fixed_points(mpc, attention, bits):
         o, s = call(*(dev(mpc, x[n]) for n in ("q", "k", "v")), decay.cuda(), dev_all(mpc, x["mat"]), dev(mpc, x["state"]))
         ln.sync()
         equal(mpc, o, w_o, "o"); equal(mpc, s, w_s, "state")
+    ln.close()
+
+
+@pytest.mark.parametrize("call", ["prompt", "step", "bias gradient"])
+@pytest.mark.parametrize("size", [(1, 1, 1, 1, 1), (1, 70, 3, 40, 65), (2, 130, 2, 128, 128)])
+def test_workspaces_of_exactly_the_queried_size(mpc, attention, call, size):
+    from test_gpu_workspace_bounds import Guarded
+    B, T, H, dk, dv = size
+    rng, L = np.random.default_rng(T), mpc.lib()
+    need = {"prompt": lambda: L.mpc_linear_attention_workspace_bytes(*size), "step": lambda: L.mpc_linear_attention_step_workspace_bytes(B, H, dk, dv),
+            "bias gradient": lambda: L.mpc_position_bias_grad_workspace_bytes(B, H, T, T, 5)}[call]()
+    g = Guarded(mpc, need)
+    g.lane._ws_bytes = need                                  # not to be grown
+    decay = attention.decay_powers([0.9, 0.97, 1.0][:H])
+    if call == "bias gradient":
+        x, m = inputs.masks(rng, B, H, T, T), rng.integers(-1, 5, 2 * T - 1).astype(np.int32)
+        grad, _ = g.lane.position_bias_grad(dev(mpc, x), mpc.to_device(m), 5)
+        got, want = (grad,), (plain.position_bias_grad(x, m, 5)[0],)
+    else:
+        d = inputs.prompt(rng, B, H, T, dk, dv) if call == "prompt" else inputs.one_token(rng, B, H, dk, dv)
+        run, form = (g.lane.linear_attention, plain.linear_attention) if call == "prompt" else (g.lane.linear_attention_step, plain.step)
+        got = run(*(dev(mpc, d[n]) for n in ("q", "k", "v")), decay.cuda(), dev_all(mpc, d["mat"]), dev(mpc, d["state"]))
+        want = form(d["q"], d["k"], d["v"], decay.numpy(), d["mat"], d["state"])
+    g.check()
+    for a, w in zip(got, want):
+        equal(mpc, a, w, call)
+
+
+def test_calls_follow_the_lanes_stream(mpc, attention):
+    """Inputs made by torch right before the call, ordered by wait_torch alone."""
+    rng = np.random.default_rng(13)
+    ln = mpc.Lane(0)
+    d = inputs.one_token(rng, 2, 3, 33, 20)
+    decay = attention.decay_powers([0.9, 0.97, 1.0])
+    want = plain.step(d["q"], d["k"], d["v"], decay.numpy(), d["mat"], d["state"])
+    host = [dev(mpc, d[n]) for n in ("q", "k", "v", "state")]
+    mat, dd = dev_all(mpc, d["mat"]), decay.cuda()
+    slow = torch.randn(4096, 4096, device="cuda:0")
+    torch.cuda.synchronize()
+    for _ in range(8):
+        slow = slow @ slow * 1e-3
+    late = [tuple(w + 0 * slow[0, :1].long() for w in pair) for pair in host]          # written behind the products
+    ln.wait_torch()
+    o, s = ln.linear_attention_step(*late[:3], dd, mat, late[3])
+    ln.sync()
+    equal(mpc, o, want[0]); equal(mpc, s, want[1])
     ln.close()
 
 
