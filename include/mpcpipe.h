@@ -531,7 +531,8 @@ int mpc_maxpool2x2_backward(mpc_ctx* ctx, mpc_cshare g, mpc_cshare s1, mpc_cshar
  * mpc_position_bias_grad: table_grad[u][h] = sum of g[b][h][i][j] over b and all pairs of bucket u (written, not added to);
  * scores_grad (both NULL to skip; may be g itself) = g, zero at masked pairs.  Sums mod 2^64 are exact: the result does not
  * depend on their order.  Workspace: the query.
- * MPC_ERANGE: n_buckets > MPC_MAX_BUCKETS, or sizes beyond 2^31. */
+ * MPC_ERANGE: n_buckets > MPC_MAX_BUCKETS, Tq + Tk, B * H or 2 * H * n_buckets near 2^31, more than 2^24 tiles (of 4096 pairs at most,
+ * each within a matrix) or, for the gradient, 2^25 entries of the table. */
 #define MPC_MAX_BUCKETS 4096
 int mpc_position_bias(mpc_ctx* ctx, mpc_cshare scores, mpc_cshare table, const int32_t* buckets, mpc_share out,
                       int B, int H, int Tq, int Tk, int n_buckets);
@@ -545,7 +546,8 @@ int mpc_position_bias_grad(mpc_ctx* ctx, mpc_cshare g, const int32_t* buckets, m
  * [N][ceil(K / group)] with scale_bits fraction bits in [0, 31]; the product is rescaled by them (the local truncation of
  * mpc_truncate), so z has the fixed point of x.  group: 32, 64 or a multiple of 128.  Linear in the shares with public
  * factors, so each party works alone: no triple, no exchange.  Workspace: the query (nothing for small products).  A call reads
- * the weights once for every eight rows of x.  MPC_ERANGE: K > MPC_MAX_K_TOTAL, M > 65535. */
+ * the weights once for every eight rows of x, small products once for every four.  MPC_ERANGE: K > MPC_MAX_K_TOTAL, M > 65535,
+ * N > 2^25. */
 size_t mpc_matvec4_workspace_bytes(int M, int K, int N);
 int mpc_matvec4(mpc_ctx* ctx, mpc_cshare x, const uint8_t* w, const int32_t* scales, mpc_share z,
                 int M, int K, int N, int group, int scale_bits);
@@ -571,8 +573,8 @@ int mpc_matvec4(mpc_ctx* ctx, mpc_cshare x, const uint8_t* w, const int32_t* sca
  *     a_s [BH][chunks][dk][dv] (mask of the state before each chunk);
  *     c_p [BH][T][64] of a_q a_k^T, c_u [BH][chunks][dk][dv] of a_kd^T a_v, c_o [BH][T][dv] of a_w a_v + a_qd a_s
  *   step: a_q, a_k [BH][dk], a_v [BH][dv], a_s [BH][dk][dv] (mask of S'); c_u [BH][dk][dv] of a_k a_v^T, c_o [BH][dv] of a_q a_s
- * MPC_ERANGE: dk or dv beyond MPC_ATTENTION_MAX_D, frac_bits > 30, B * H beyond 2^31, an input token stride of a prompt beyond
- * MPC_ATTENTION_MAX_TOKEN_STRIDE.  Workspace: the queries. */
+ * MPC_ERANGE: dk or dv beyond MPC_ATTENTION_MAX_D, frac_bits > 30, H beyond 2^31 / 65, B * H * chunks beyond 2^31 / 5, an input
+ * token stride of a prompt beyond MPC_ATTENTION_MAX_TOKEN_STRIDE.  Workspace: the queries. */
 #define MPC_ATTENTION_CHUNK 64
 #define MPC_ATTENTION_MAX_D 128
 #define MPC_ATTENTION_MAX_TOKEN_STRIDE 4194303     /* of q, k, v of a prompt, in words */

@@ -43,8 +43,10 @@ def relative_buckets(Tq: int, Tk: int, n_buckets: int, max_distance: int, causal
 def decay_powers(decay, frac_bits: int = 16) -> torch.Tensor:
     """Powers 0..64 of every head's decay in [0, 1] as fixed point, int32 [H, 65]."""
     d = torch.as_tensor(decay, dtype=torch.float64)
-    if d.ndim != 1 or bool(((d < 0) | (d > 1)).any()):
+    if d.ndim != 1 or not bool(((d >= 0) & (d <= 1)).all()):
         raise ValueError("one decay in [0, 1] for each head expected")
+    if not 0 <= frac_bits <= 30:
+        raise ValueError("frac_bits in [0, 30] expected: a decay of one has to fit 31 bits")
     return torch.round(d[:, None] ** torch.arange(mpc.ATTENTION_CHUNK + 1) * 2.0 ** frac_bits).to(torch.int32)
 
 
@@ -61,6 +63,8 @@ def quantize4(w: torch.Tensor, group: int, scale_bits: int = 20):
     """Nearest 4-bit form of real weights [N, K]: (packed weights, int32 scales [N, ceil(K / group)]); a group's scale is its
     largest magnitude over 7."""
     N, K = w.shape
+    if group <= 0 or not bool((w.abs().double() * 2.0 ** scale_bits / 7 < 2 ** 31 - 1).all()):
+        raise ValueError("a positive group and finite weights whose scales fit 31 bits expected")
     g = torch.nn.functional.pad(w.double(), (0, -K % group)).view(N, -1, group)
     scales = torch.round(g.abs().amax(-1) / 7 * 2.0 ** scale_bits).clamp(min=1, max=2 ** 31 - 1)
     q = torch.round(g / (scales[..., None] * 2.0 ** -scale_bits)).clamp(-8, 7).view(N, -1)[:, :K]

@@ -22,6 +22,13 @@ static inline bool overlap(const void* p, size_t np, const void* q, size_t nq)
     const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
     return a < b + nq && b < a + np;
 }
+// a launch has fewer than 2^32 threads
+static inline bool launchable(size_t blocks, size_t threads) { return blocks <= UINT32_MAX / threads; }
+// an output apart from a public array
+static inline bool apart(const mpc_share& out, size_t n_out, const void* p, size_t n)
+{
+    return !overlap(out.p[0], n_out, p, n) && !overlap(out.p[1], n_out, p, n);
+}
 // every output apart from every input, other than an output that is the very array of its own party's input
 static inline bool outputs_apart(const mpc_share& out, size_t n_out, const mpc_cshare& in, size_t n_in, bool may_be_same)
 {

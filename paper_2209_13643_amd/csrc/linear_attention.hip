@@ -597,7 +597,8 @@ mpc_cshare seen(const mpc_share& s) { return mpc_cshare{ { s.p[0], s.p[1] } }; }
 int shape_ok(mpc_ctx* c, int B, int T, int H, int dk, int dv)
 {
     if (B <= 0 || T <= 0 || H <= 0 || dk <= 0 || dv <= 0) return MPC_EINVAL;
-    if (dk > MPC_ATTENTION_MAX_D || dv > MPC_ATTENTION_MAX_D || (long long)B * H > INT32_MAX || T > INT32_MAX - kChunk) return MPC_ERANGE;
+    if (dk > MPC_ATTENTION_MAX_D || dv > MPC_ATTENTION_MAX_D || H > INT32_MAX / (kChunk + 1) || T > INT32_MAX - kChunk) return MPC_ERANGE;
+    if (((long long)T + kChunk - 1) / kChunk * B * H > INT32_MAX / 5) return MPC_ERANGE;      // jobs of a launch
     return c && c->frac_bits > 30 ? MPC_ERANGE : MPC_OK;       // a decay of one has to fit 31 bits
 }
 
@@ -638,7 +639,6 @@ int mpc_linear_attention(mpc_ctx* c, const mpc_attention_operands* x, const mpc_
     if (!strides_in(sq) || !strides_in(sk) || !strides_in(sv) || !strides_out(so, B, T, H, dv)) return MPC_EINVAL;
     if (far_tokens(sq) || far_tokens(sk) || far_tokens(sv)) return MPC_ERANGE;
     const ChunkPlan p = plan(B, T, H, dk, dv);
-    if ((long long)B * H * p.chunks * 5 > INT32_MAX) return MPC_ERANGE;      // jobs of a launch
     const size_t n_o = extent(so, B, T, H, dv) * 8, n_s = (size_t)B * H * dk * dv * 8;
     const size_t BHT = (size_t)B * H * T * 8;
     const size_t sizes[] = { BHT * dk, BHT * dk, BHT * dk, BHT * dk, BHT * dv, BHT * kChunk, p.u * 8, BHT * kChunk, p.u * 8, BHT * dv };
@@ -652,7 +652,9 @@ int mpc_linear_attention(mpc_ctx* c, const mpc_attention_operands* x, const mpc_
         for (int i = 0; i < 10; ++i) if (!outputs_apart(out, n, *mats[i], sizes[i], false)) return MPC_EINVAL;
         if (state.p[0] && !outputs_apart(out, n, state, n_s, pass == 1)) return MPC_EINVAL;
     }
-    if (state_out.p[0] && !outputs_apart(o, n_o, seen(state_out), n_s, false)) return MPC_EINVAL;
+    const size_t n_decay = (size_t)H * (kChunk + 1) * 4;
+    if (!apart(o, n_o, decay, n_decay)) return MPC_EINVAL;
+    if (state_out.p[0] && (!outputs_apart(o, n_o, seen(state_out), n_s, false) || !apart(state_out, n_s, decay, n_decay))) return MPC_EINVAL;
 
     ChunkArgs a{};
     a.q = rows_of(q, sq); a.k = rows_of(k, sk); a.v = rows_of(v, sv);
@@ -699,7 +701,8 @@ int mpc_linear_attention_step(mpc_ctx* c, const mpc_attention_operands* x, const
         for (int i = 0; i < 6; ++i) if (!outputs_apart(out, n, *mats[i], sizes[i], false)) return MPC_EINVAL;
         if (!outputs_apart(out, n, state, n_s, pass == 1)) return MPC_EINVAL;
     }
-    if (!outputs_apart(o, n_o, seen(state_out), n_s, false)) return MPC_EINVAL;
+    const size_t n_decay = (size_t)H * (kChunk + 1) * 4;
+    if (!outputs_apart(o, n_o, seen(state_out), n_s, false) || !apart(o, n_o, decay, n_decay) || !apart(state_out, n_s, decay, n_decay)) return MPC_EINVAL;
     if (!c->ws || c->ws_bytes < mpc_linear_attention_step_workspace_bytes(B, H, dk, dv)) return MPC_ENOMEM;
     StepArgs a{};
     a.q = rows_of(q, sq); a.k = rows_of(k, sk); a.v = rows_of(v, sv);
@@ -709,8 +712,7 @@ int mpc_linear_attention_step(mpc_ctx* c, const mpc_attention_operands* x, const
     }
     a.ob = so.batch; a.oh = so.head; a.decay = decay; a.box = reinterpret_cast<u64*>(c->ws);
     a.B = B; a.H = H; a.dk = dk; a.dv = dv; a.bits = c->frac_bits; a.slices = (dv + kSlice - 1) / kSlice;
-    const long long jobs = (long long)B * H * a.slices;
-    if (jobs > INT32_MAX) return MPC_ERANGE;
+    const long long jobs = (long long)B * H * a.slices;           // at most four slices to a head
     MPC_TRY(lane_first(c));
     k_step<<<dim3((unsigned)(jobs < kStepBoxes ? jobs : kStepBoxes)), 256, 0, c->s[0]>>>(a);
     MPC_HIP(c, hipGetLastError());

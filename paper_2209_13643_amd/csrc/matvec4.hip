@@ -23,6 +23,7 @@ struct MatvecArgs {
 };
 
 constexpr int kBlock = 256;                   // columns that a wave takes at a time
+constexpr int kMostN = 1 << 25;               // 2^21 workgroups of up to 1024 threads
 constexpr int most_waves(int mt) { return mt == 1 ? 16 : 8; }
 
 // Whether the digits of x are made once, by a launch of their own, instead of by every workgroup for itself.  us with and without:
@@ -205,7 +206,7 @@ extern "C" {
 
 size_t mpc_matvec4_workspace_bytes(int M, int K, int N)
 {
-    if (M <= 0 || K <= 0 || N <= 0 || K > MPC_MAX_K_TOTAL || M > 65535 || !digits_in_memory(M, K, N)) return 0;
+    if (M <= 0 || K <= 0 || N <= 0 || K > MPC_MAX_K_TOTAL || M > 65535 || N > kMostN || !digits_in_memory(M, K, N)) return 0;
     return (size_t)M * ((K + kBlock - 1) / kBlock) * 4096;
 }
 
@@ -216,15 +217,15 @@ int mpc_matvec4(mpc_ctx* c, mpc_cshare x, const uint8_t* w, const int32_t* scale
     if (group <= 0 || (group != 32 && group != 64 && group % 128)) return MPC_EINVAL;
     if (((uintptr_t)w & 15) || ((uintptr_t)scales & 3)) return MPC_EINVAL;
     for (int i = 0; i < 2; ++i) if (!x.p[i] || !z.p[i]) return MPC_EINVAL;
-    if (K > MPC_MAX_K_TOTAL || M > 65535) return MPC_ERANGE;
+    if (K > MPC_MAX_K_TOTAL || M > 65535 || N > kMostN) return MPC_ERANGE;
     MatvecArgs q{};
     q.groups = (K + group - 1) / group; q.row_bytes = (K + 31) / 32 * 16;
     const size_t out = (size_t)M * N * 8;
     if (!outputs_apart(z, out, x, (size_t)M * K * 8, false)) return MPC_EINVAL;
     for (int i = 0; i < 2; ++i) {
         q.x[i] = x.p[i]; q.z[i] = z.p[i];
-        if (overlap(z.p[i], out, w, (size_t)N * q.row_bytes) || overlap(z.p[i], out, scales, (size_t)N * q.groups * 4)) return MPC_EINVAL;
     }
+    if (!apart(z, out, w, (size_t)N * q.row_bytes) || !apart(z, out, scales, (size_t)N * q.groups * 4)) return MPC_EINVAL;
     q.w = w; q.scales = scales; q.M = M; q.K = K; q.N = N; q.group = group; q.shift = scale_bits;
     q.blocks = (K + kBlock - 1) / kBlock;
     if (digits_in_memory(M, K, N)) {

@@ -174,7 +174,8 @@ void share_out(BiasArgs& q)
 int bias_shape(BiasArgs& q, int B, int H, int Tq, int Tk, int n_buckets)
 {
     if (B <= 0 || H <= 0 || Tq <= 0 || Tk <= 0 || n_buckets <= 0) return MPC_EINVAL;
-    if (n_buckets > MPC_MAX_BUCKETS || (long long)Tq + Tk - 1 > INT32_MAX || (long long)B * H > INT32_MAX || 2ll * H * n_buckets > INT32_MAX) return MPC_ERANGE;
+    if (n_buckets > MPC_MAX_BUCKETS || (long long)Tq + Tk > INT32_MAX - 1024 ||      // diagonals are counted in int, a workgroup's 1024 at a time
+        (long long)B * H > INT32_MAX || 2ll * H * n_buckets > INT32_MAX) return MPC_ERANGE;
     q.B = B; q.H = H; q.BH = (unsigned)B * H; q.Tq = Tq; q.Tk = Tk; q.n_buckets = n_buckets;
     return MPC_OK;
 }
@@ -198,13 +199,13 @@ int mpc_position_bias(mpc_ctx* c, mpc_cshare x, mpc_cshare table, const int32_t*
     if (!c || !buckets) return MPC_EINVAL;
     for (int i = 0; i < 2; ++i) if (!x.p[i] || !table.p[i] || !out.p[i]) return MPC_EINVAL;
     MPC_TRY(bias_shape(q, B, H, Tq, Tk, n_buckets));
-    const size_t bytes = (size_t)q.BH * Tq * Tk * 8;
-    if (!outputs_apart(out, bytes, x, bytes, true) || !outputs_apart(out, bytes, table, (size_t)n_buckets * H * 8, false)) return MPC_EINVAL;
     q.cols = Tk < kCols ? Tk : kCols;
     q.rows = kTilePairs / q.cols; if (q.rows > kRows) q.rows = kRows; if (q.rows > q.Tq) q.rows = q.Tq;
     q.row_tiles = (q.Tq + q.rows - 1) / q.rows; q.col_tiles = (q.Tk + q.cols - 1) / q.cols;
-    const size_t grid = 2 * (size_t)q.BH * q.row_tiles * q.col_tiles;
-    if (grid > INT32_MAX) return MPC_ERANGE;
+    const size_t grid = 2 * (size_t)q.BH * q.row_tiles * q.col_tiles, bytes = (size_t)q.BH * Tq * Tk * 8;
+    if (!launchable(grid, kThreads)) return MPC_ERANGE;
+    if (!apart(out, bytes, buckets, ((size_t)Tq + Tk - 1) * 4)) return MPC_EINVAL;
+    if (!outputs_apart(out, bytes, x, bytes, true) || !outputs_apart(out, bytes, table, (size_t)n_buckets * H * 8, false)) return MPC_EINVAL;
     for (int i = 0; i < 2; ++i) { q.x[i] = x.p[i]; q.table[i] = table.p[i]; q.out[i] = out.p[i]; }
     q.buckets = buckets;
     MPC_TRY(lane_first(c));
@@ -220,13 +221,14 @@ int mpc_position_bias_grad(mpc_ctx* c, mpc_cshare g, const int32_t* buckets, mpc
     if (!c || !buckets || !scores_grad.p[0] != !scores_grad.p[1]) return MPC_EINVAL;
     for (int i = 0; i < 2; ++i) if (!g.p[i] || !table_grad.p[i]) return MPC_EINVAL;
     MPC_TRY(bias_shape(q, B, H, Tq, Tk, n_buckets));
-    const size_t bytes = (size_t)q.BH * Tq * Tk * 8, table_bytes = (size_t)n_buckets * H * 8;
-    const bool scores = scores_grad.p[0] != nullptr;
-    if (!outputs_apart(table_grad, table_bytes, g, bytes, false)) return MPC_EINVAL;
-    if (scores && (!outputs_apart(scores_grad, bytes, g, bytes, true) ||
-                   !outputs_apart(table_grad, table_bytes, mpc_cshare{ { scores_grad.p[0], scores_grad.p[1] } }, bytes, false))) return MPC_EINVAL;
     share_out(q);
-    if ((size_t)q.row_tiles * q.col_tiles * q.splits > INT32_MAX || 2 * (size_t)H * q.parts > INT32_MAX) return MPC_ERANGE;
+    const size_t items = (size_t)q.row_tiles * q.col_tiles * q.splits, sums = (2 * (size_t)H * n_buckets + 3) / 4;
+    if (items > INT32_MAX || !launchable(2 * (size_t)H * q.parts, 64 * q.waves) || !launchable(sums, kThreads)) return MPC_ERANGE;
+    const size_t bytes = (size_t)q.BH * Tq * Tk * 8, table_bytes = (size_t)n_buckets * H * 8, public_bytes = ((size_t)Tq + Tk - 1) * 4;
+    const bool scores = scores_grad.p[0] != nullptr;
+    if (!outputs_apart(table_grad, table_bytes, g, bytes, false) || !apart(table_grad, table_bytes, buckets, public_bytes)) return MPC_EINVAL;
+    if (scores && (!apart(scores_grad, bytes, buckets, public_bytes) || !outputs_apart(scores_grad, bytes, g, bytes, true) ||
+                   !outputs_apart(table_grad, table_bytes, mpc_cshare{ { scores_grad.p[0], scores_grad.p[1] } }, bytes, false))) return MPC_EINVAL;
     WsAlloc ws(c->ws, c->ws_bytes);
     q.partial = ws.take<u64>(2 * (size_t)H * n_buckets * q.parts);
     if (!ws.ok) return MPC_ENOMEM;
@@ -237,7 +239,7 @@ int mpc_position_bias_grad(mpc_ctx* c, mpc_cshare g, const int32_t* buckets, mpc
     const size_t lds = (size_t)n_buckets * 8;
     if (scores) k_position_bias_grad<true><<<grid, block, lds, c->s[0]>>>(q);
     else k_position_bias_grad<false><<<grid, block, lds, c->s[0]>>>(q);
-    k_position_bias_sums<<<dim3((unsigned)((2 * (size_t)H * n_buckets + 3) / 4)), kThreads, 0, c->s[0]>>>(q);
+    k_position_bias_sums<<<dim3((unsigned)sums), kThreads, 0, c->s[0]>>>(q);
     MPC_HIP(c, hipGetLastError());
     return lane_fanout(c);
 }

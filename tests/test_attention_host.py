@@ -229,6 +229,38 @@ def test_refusals(tmp_path):
     assert r["frac"] == [R, R] and r["null"] == [E, E, E, E] and r["launched by refused calls"] == []
 
 
+SIZES_AND_OVERLAPS = r'''
+result["bias"] = [bias(B=1 << 24, H=1, Tq=1, Tk=1), bias(B=1, H=1, Tq=1, Tk=(1 << 31) - 1), bias(o=x, m=x.p[0]), bias(o=x, m=x.p[1] + 16)]
+result["grad"] = [grad(B=1, H=1, Tq=1, Tk=(1 << 31) - 2), grad(H=1 << 14, n=4096), grad(B=1, H=1 << 25, Tq=1, Tk=1, n=1), grad(t=x, m=x.p[1]), grad(s=x, m=x.p[0])]
+result["matvec4"] = [mv(M=1, K=1, N=(1 << 25) + 1), mv(M=1, K=1, N=(1 << 31) - 1)]
+result["prompt"] = [prompt(B=1, H=1 << 26, T=1, dk=1, dv=1), prompt(B=1, H=1, T=(1 << 31) - 1), prompt(o=x, decay=x.p[0]), prompt(out=x, decay=x.p[1])]
+result["step"] = [step(B=1, H=1 << 26, dk=1, dv=1)]
+result["queries"] = [lib.mpc_linear_attention_workspace_bytes(1 << 15, (1 << 31) - 100, 1 << 15, 128, 128), lib.mpc_matvec4_workspace_bytes(8, 64, (1 << 31) - 1)]
+result["refused calls launched"] = launches()
+'''
+
+
+def test_sizes_beyond_a_launch_and_outputs_on_public_arrays(tmp_path):
+    r = fake_hip.run(tmp_path, REFUSALS + "lib.mpc_ctx_set_workspace(ctx, array(big), big); launches()\n" + SIZES_AND_OVERLAPS)
+    E, R = -1, -4
+    assert r["bias"] == [R, R, E, E] and r["grad"] == [R, R, R, E, E] and r["matvec4"] == [R, R]
+    assert r["prompt"] == [R, R, E, E] and r["step"] == [R]
+    assert r["queries"] == [0, 0] and r["refused calls launched"] == []
+
+
+def test_helpers_refuse_what_is_not_finite():
+    for bad in [[float("nan")], [0.5, float("inf")]]:
+        with pytest.raises(ValueError):
+            attention.decay_powers(bad)
+    with pytest.raises(ValueError):
+        attention.decay_powers([0.5], 31)
+    for bad in [float("nan"), float("inf"), -1e6]:
+        with pytest.raises(ValueError):
+            attention.quantize4(torch.tensor([[0.5, bad]]), 32)
+    with pytest.raises(ValueError):
+        attention.quantize4(torch.ones(2, 2), 0)
+
+
 def test_workspace_queries_refuse():
     from paper_2209_13643_amd import mpc
     L = mpc.lib()
