@@ -420,7 +420,7 @@ __global__ __launch_bounds__(kThreads) void k_chunk_out(ChunkArgs q)
         u64 z0[8], z1[8];
         each_word(p, [&](int r, int i, int j) {
             const unsigned o = min(i, L - 1) * q.dv + min(n0 + j, q.dv - 1);
-            z0[r] = (q.part[0] + at * q.dv)[o]; z1[r] = (q.part[1] + at * q.dv)[o];
+            z0[r] = __builtin_nontemporal_load(q.part[0] + at * q.dv + o); z1[r] = __builtin_nontemporal_load(q.part[1] + at * q.dv + o);
         });
         for (int k0 = 0; k0 < q.dk; k0 += 64) {
             const Place ps = anew(p);
@@ -446,8 +446,8 @@ __global__ __launch_bounds__(kThreads) void k_chunk_out(ChunkArgs q)
         each_word(anew(p), [&](int r, int i, int j) {
             if (i >= L || n0 + j >= q.dv) return;
             const long long o = i * q.ot;
-            (q.o[0] + to)[o + j] = rescaled<0>(z0[r], q.bits);
-            (q.o[1] + to)[o + j] = rescaled<1>(z1[r], q.bits);
+            __builtin_nontemporal_store(rescaled<0>(z0[r], q.bits), q.o[0] + to + o + j);
+            __builtin_nontemporal_store(rescaled<1>(z1[r], q.bits), q.o[1] + to + o + j);
         });
     }
 }
