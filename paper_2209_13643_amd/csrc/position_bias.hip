@@ -16,7 +16,8 @@ constexpr int kRows = 512;               // rows of a tile, at most
 constexpr int kTilePairs = 4096;         // (i, j) pairs of a tile, at most
 
 constexpr int kAtOnce = 8;               // rows of the gradient on their way at a time
-constexpr size_t kEnough = 2048;         // workgroups
+constexpr size_t kEnough = 2048;         // workgroups; of the gradient up to four times as many
+constexpr int kFewBuckets = 256;         // with more, a workgroup's partial sums cost too much for that
 constexpr unsigned kMostWaves = 8;       // of them
 
 struct BiasArgs {
@@ -70,7 +71,9 @@ __global__ __launch_bounds__(kThreads) void k_position_bias(BiasArgs q)
 // A wave takes 128 diagonals of a block of rows, two to a lane, through all matrices of its workgroup, and keeps their sums in
 // registers: a row's words are read side by side, and one sum a diagonal goes to its bucket in LDS; the workgroups' buckets are added
 // up by a second launch (atomics on the table would need a launch ahead to clear it).  Diagonal k of a block of `rows` rows
-// from i0 on holds the pairs (i0 + r, r + k - (rows - 1)).
+// from i0 on holds the pairs (i0 + r, r + k - (rows - 1)).  Row blocks follow one another: shares of diagonals that do not read
+// (masked ones) and those that do would otherwise go to different dies (18 x 1121 x 1121, causal: 162 us, so 135).
+// 96 x 512 x 512: 77 us with the sums' launch, 5.2 TB/s.
 template <bool SCORES>
 __global__ __launch_bounds__(64 * kMostWaves) void k_position_bias_grad(BiasArgs q)
 {
@@ -80,7 +83,7 @@ __global__ __launch_bounds__(64 * kMostWaves) void k_position_bias_grad(BiasArgs
     __syncthreads();
     const unsigned items = q.row_tiles * q.col_tiles * q.splits;
     for (unsigned item = part; item < items; item += q.parts) {
-        const unsigned dt = item % q.col_tiles, it = item / q.col_tiles % q.row_tiles, b0 = item / q.col_tiles / q.row_tiles * q.batches;
+        const unsigned it = item % q.row_tiles, dt = item / q.row_tiles % q.col_tiles, b0 = item / q.row_tiles / q.col_tiles * q.batches;
         const unsigned i0 = it * q.rows;
         const int rows = min(q.Tq - i0, q.rows), cols = q.Tk;
         const unsigned nb = min(q.B - b0, q.batches);
@@ -151,16 +154,19 @@ __global__ __launch_bounds__(kThreads) void k_position_bias_sums(BiasArgs q)
     if (lane == 0) q.grad[ph / q.H][(size_t)u * q.H + ph % q.H] = s;
 }
 
-// How the gradient is shared out: blocks of 32 rows, of fewer where that makes too few items; as many matrices to an item as leave
-// enough; and workgroups (parts) for each party and head.
+// How the gradient is shared out: blocks of 32 rows, of fewer where that makes too few items, and even shares of their diagonals; as
+// many matrices to an item as leave enough; and workgroups (parts) for each party and head, one to an item up to four times
+// enough.  With a fixed number, some of two items, and a second share of few diagonals, 16 x 1175 x 1175 with the scores' gradient
+// took 206 us instead of 129, 24 x 1500 x 1500 without it 183 instead of 154.
 void share_out(BiasArgs& q)
 {
     size_t one = 0;
     for (q.rows = 32; ; q.rows /= 2) {
         if (q.rows > q.Tq) q.rows = q.Tq;
         const size_t diagonals = (size_t)q.rows + q.Tk - 1;
-        q.waves = (unsigned)std::min<size_t>((diagonals + 127) / 128, kMostWaves);
-        q.row_tiles = (q.Tq + q.rows - 1) / q.rows; q.col_tiles = (unsigned)((diagonals + 128 * q.waves - 1) / (128 * q.waves));
+        const unsigned waves = (unsigned)((diagonals + 127) / 128);
+        q.row_tiles = (q.Tq + q.rows - 1) / q.rows; q.col_tiles = (waves + kMostWaves - 1) / kMostWaves;
+        q.waves = (waves + q.col_tiles - 1) / q.col_tiles;
         one = 2 * (size_t)q.H * q.row_tiles * q.col_tiles;
         if (one * q.B >= kEnough || q.rows <= 8) break;
     }
@@ -168,13 +174,14 @@ void share_out(BiasArgs& q)
     q.batches = (unsigned)((q.B + splits - 1) / splits);
     q.splits = (q.B + q.batches - 1) / q.batches;
     const size_t items = (size_t)q.row_tiles * q.col_tiles * q.splits;
-    q.parts = (unsigned)std::min<size_t>(items, (kEnough + 2 * q.H - 1) / (2 * q.H));
+    const size_t most = ((q.n_buckets > kFewBuckets ? kEnough : 4 * kEnough) + 2 * q.H - 1) / (2 * q.H), each = (items + most - 1) / most;
+    q.parts = (unsigned)((items + each - 1) / each);
 }
 
 int bias_shape(BiasArgs& q, int B, int H, int Tq, int Tk, int n_buckets)
 {
     if (B <= 0 || H <= 0 || Tq <= 0 || Tk <= 0 || n_buckets <= 0) return MPC_EINVAL;
-    if (n_buckets > MPC_MAX_BUCKETS || (long long)Tq + Tk > INT32_MAX - 1024 ||      // diagonals are counted in int, a workgroup's 1024 at a time
+    if (n_buckets > MPC_MAX_BUCKETS || (long long)Tq + Tk > INT32_MAX - 2048 ||      // diagonals are counted in int, up to 1024 of a workgroup at a time
         (long long)B * H > INT32_MAX || 2ll * H * n_buckets > INT32_MAX) return MPC_ERANGE;
     q.B = B; q.H = H; q.BH = (unsigned)B * H; q.Tq = Tq; q.Tk = Tk; q.n_buckets = n_buckets;
     return MPC_OK;
