@@ -10,7 +10,8 @@
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;
+constexpr int kSumThreads = 256;
 constexpr int kCols = 1024;              // columns of a tile, at most
 constexpr int kRows = 512;               // rows of a tile, at most
 constexpr int kTilePairs = 4096;         // (i, j) pairs of a tile, at most
@@ -29,15 +30,18 @@ struct BiasArgs {
     u64* partial;                                   // gradient: [party][H][bucket][part]
 };
 
-// 96 x 512 x 512: 134 us, 6.0 TB/s; with ordinary accesses 148, and 157 with tiles of twice the size.
-// What the distances of a tile add, and where nothing is kept: entry k is distance j - i = j0 - i0 - (rows - 1) + k.
+// A workgroup's tile: what its distances add, and where nothing is kept, is made once in LDS (entry k is distance j - i =
+// j0 - i0 - (rows - 1) + k), then a thread moves two pairs at a time.  96 x 512 x 512: 130 us, 6.2 TB/s; with 256 threads 134 (and
+// with ordinary accesses 10 % more), with 1024 and tiles of twice the size 136.  The tiles of a column follow one another: a matrix
+// of two columns had its left tiles, all of a causal mask's reads, on every other die (24 x 1500 x 1500: 317 us, so 255, and 241
+// with 512 threads).
 __global__ __launch_bounds__(kThreads) void k_position_bias(BiasArgs q)
 {
     // (word, kept mask); rows + cols is largest at either end of cols: kCols + kTilePairs / kCols, kRows + kTilePairs / kRows
     __shared__ ulonglong2 by_distance[kCols + kTilePairs / kCols];
     unsigned t = blockIdx.x;
-    const unsigned jt = t % q.col_tiles; t /= q.col_tiles;
     const unsigned it = t % q.row_tiles; t /= q.row_tiles;
+    const unsigned jt = t % q.col_tiles; t /= q.col_tiles;
     const unsigned bh = t % q.BH, party = t / q.BH, h = bh % q.H;
     const unsigned i0 = it * q.rows, j0 = jt * q.cols;
     const unsigned rows = q.Tq - i0 < q.rows ? q.Tq - i0 : q.rows, cols = q.Tk - j0 < q.cols ? q.Tk - j0 : q.cols;
@@ -142,9 +146,9 @@ __global__ __launch_bounds__(64 * kMostWaves) void k_position_bias_grad(BiasArgs
 }
 
 // the workgroups' sums of a bucket and head, a wave each
-__global__ __launch_bounds__(kThreads) void k_position_bias_sums(BiasArgs q)
+__global__ __launch_bounds__(kSumThreads) void k_position_bias_sums(BiasArgs q)
 {
-    const unsigned n = 2 * q.H * (unsigned)q.n_buckets, at = blockIdx.x * (kThreads / 64) + threadIdx.x / 64, lane = threadIdx.x % 64;
+    const unsigned n = 2 * q.H * (unsigned)q.n_buckets, at = blockIdx.x * (kSumThreads / 64) + threadIdx.x / 64, lane = threadIdx.x % 64;
     if (at >= n) return;
     u64 s = 0;
     for (unsigned i = lane; i < q.parts; i += 64) s += q.partial[(size_t)at * q.parts + i];
@@ -229,8 +233,8 @@ int mpc_position_bias_grad(mpc_ctx* c, mpc_cshare g, const int32_t* buckets, mpc
     for (int i = 0; i < 2; ++i) if (!g.p[i] || !table_grad.p[i]) return MPC_EINVAL;
     MPC_TRY(bias_shape(q, B, H, Tq, Tk, n_buckets));
     share_out(q);
-    const size_t items = (size_t)q.row_tiles * q.col_tiles * q.splits, sums = (2 * (size_t)H * n_buckets + 3) / 4;
-    if (items > INT32_MAX || !launchable(2 * (size_t)H * q.parts, 64 * q.waves) || !launchable(sums, kThreads)) return MPC_ERANGE;
+    const size_t items = (size_t)q.row_tiles * q.col_tiles * q.splits, sums = (2 * (size_t)H * n_buckets + kSumThreads / 64 - 1) / (kSumThreads / 64);
+    if (items > INT32_MAX || !launchable(2 * (size_t)H * q.parts, 64 * q.waves) || !launchable(sums, kSumThreads)) return MPC_ERANGE;
     const size_t bytes = (size_t)q.BH * Tq * Tk * 8, table_bytes = (size_t)n_buckets * H * 8, public_bytes = ((size_t)Tq + Tk - 1) * 4;
     const bool scores = scores_grad.p[0] != nullptr;
     if (!outputs_apart(table_grad, table_bytes, g, bytes, false) || !apart(table_grad, table_bytes, buckets, public_bytes)) return MPC_EINVAL;
@@ -246,7 +250,7 @@ int mpc_position_bias_grad(mpc_ctx* c, mpc_cshare g, const int32_t* buckets, mpc
     const size_t lds = (size_t)n_buckets * 8;
     if (scores) k_position_bias_grad<true><<<grid, block, lds, c->s[0]>>>(q);
     else k_position_bias_grad<false><<<grid, block, lds, c->s[0]>>>(q);
-    k_position_bias_sums<<<dim3((unsigned)sums), kThreads, 0, c->s[0]>>>(q);
+    k_position_bias_sums<<<dim3((unsigned)sums), kSumThreads, 0, c->s[0]>>>(q);
     MPC_HIP(c, hipGetLastError());
     return lane_fanout(c);
 }
