@@ -19,16 +19,33 @@ struct MatvecArgs {
     const u64* x[2]; u64* z[2];
     const u8* w; const int32_t* scales;
     uint32_t* digits;                     // digits in memory, or none
-    int M, K, N, group, groups, row_bytes, shift, blocks;
+    u64* partial;                         // [split][row][party][N], where the columns are split over workgroups
+    int M, K, N, group, groups, row_bytes, shift, blocks, splits;
 };
 
 constexpr int kBlock = 256;                   // columns that a wave takes at a time
+constexpr int kUnits = 256, kLong = 4;
 constexpr int kMostN = 1 << 25;               // 2^21 workgroups of up to 1024 threads
 constexpr int most_waves(int mt) { return mt == 1 ? 16 : 8; }
 
 // Whether the digits of x are made once, by a launch of their own, instead of by every workgroup for itself.  us with and without:
 // 8 x 25088 x 4096 51 / 76, 16 x 4096 x 4096 33 / 44; but 4 x 4096 x 4096 12 / 12, 8 x 1024 x 4096 13 / 11, 1 x 768 x 2304 7 / 4.
 bool digits_in_memory(int M, int K, int N) { return M > 4 && (long long)M * K * N >= 1ll << 27; }
+
+// Rows of x to a workgroup.
+int rows_at_once(int M, int K, int N) { return digits_in_memory(M, K, N) ? 8 : M < 3 ? M : 4; }
+// Into how many workgroups the columns are split: few rows of the weights that are long leave most units idle, and a workgroup's
+// waves go through several blocks one after the other.  The sums are added by a launch of their own.  us without and with:
+// 1 x 25088 x 10 31 / 11, 1 x 25088 x 1000 23 / 16, 8 x 25088 x 200 44 / 23; but for more than kUnits workgroups 1 x 25088 x 4096
+// 18 / 21, and for fewer than kLong blocks to a wave 16 x 4096 x 1000 12 / 18.
+int splits_of(int M, int K, int N)
+{
+    const int mt = rows_at_once(M, K, N), blocks = (K + kBlock - 1) / kBlock, waves = most_waves(mt);
+    const long long workgroups = (N + 15ll) / 16 * ((M + mt - 1) / mt);
+    if (blocks < kLong * waves || workgroups >= kUnits) return 1;
+    const int splits = (int)((kUnits + workgroups - 1) / workgroups), most = blocks / waves;
+    return splits < most ? splits : most;
+}
 
 // The digits of a block of x in LDS, as the lanes of a product read them: for every set of G columns (kg: a quarter of them) and
 // column c = 8 party + digit, the words' bytes in the order in which a lane's weights come out of their halves, even columns
@@ -107,7 +124,8 @@ __global__ __launch_bounds__(64 * most_waves(MT)) void k_matvec4(MatvecArgs q)
         }
         return v;
     };
-    for (int block = wave; block < q.blocks; block += waves) {
+    const int per = (q.blocks + q.splits - 1) / q.splits, first = blockIdx.z * per, last = min(first + per, q.blocks);
+    for (int block = first + wave; block < last; block += waves) {
         const int k0 = block * kBlock;
         Right next = right(block, 0);
         uint32_t w[8];                                                  // [set][kBytes / 4]
@@ -180,14 +198,28 @@ __global__ __launch_bounds__(64 * most_waves(MT)) void k_matvec4(MatvecArgs q)
         const int m = t / 32, n = t % 16, p = t / 16 % 2;
         u64 v = 0;
         for (int i = 0; i < waves; ++i) v += sums[i][m][n][p];
-        if (m0 + m < q.M && n0 + n < q.N) q.z[p][(size_t)(m0 + m) * q.N + n0 + n] = rescaled(p, v, q.shift);
+        if (m0 + m >= q.M || n0 + n >= q.N) continue;
+        if (q.splits > 1) q.partial[(((size_t)blockIdx.z * q.M + m0 + m) * 2 + p) * q.N + n0 + n] = v;
+        else q.z[p][(size_t)(m0 + m) * q.N + n0 + n] = rescaled(p, v, q.shift);
     }
+}
+
+// the splits' sums
+__global__ __launch_bounds__(256) void k_matvec4_join(MatvecArgs q)
+{
+    const size_t n = 2 * (size_t)q.M * q.N, at = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= n) return;
+    const size_t m = at / q.N / 2, p = at / q.N % 2;
+    u64 v = 0;
+    for (int i = 0; i < q.splits; ++i) v += q.partial[(size_t)i * n + at];
+    q.z[p][m * q.N + at % q.N] = rescaled((int)p, v, q.shift);
 }
 
 template <int G, int MT, bool MADE> void launch(const MatvecArgs& q, hipStream_t st)
 {
     const int waves = q.blocks < most_waves(MT) ? q.blocks : most_waves(MT);
-    k_matvec4<G, MT, MADE><<<dim3((q.N + 15) / 16, (q.M + MT - 1) / MT), 64 * waves, 0, st>>>(q);
+    k_matvec4<G, MT, MADE><<<dim3((q.N + 15) / 16, (q.M + MT - 1) / MT, q.splits), 64 * waves, 0, st>>>(q);
+    if (q.splits > 1) k_matvec4_join<<<dim3((unsigned)((2 * (size_t)q.M * q.N + 255) / 256)), 256, 0, st>>>(q);
 }
 template <int G> void launch(const MatvecArgs& q, hipStream_t st)
 {
@@ -206,8 +238,9 @@ extern "C" {
 
 size_t mpc_matvec4_workspace_bytes(int M, int K, int N)
 {
-    if (M <= 0 || K <= 0 || N <= 0 || K > MPC_MAX_K_TOTAL || M > 65535 || N > kMostN || !digits_in_memory(M, K, N)) return 0;
-    return (size_t)M * ((K + kBlock - 1) / kBlock) * 4096;
+    if (M <= 0 || K <= 0 || N <= 0 || K > MPC_MAX_K_TOTAL || M > 65535 || N > kMostN) return 0;
+    const int splits = splits_of(M, K, N);
+    return (digits_in_memory(M, K, N) ? (size_t)M * ((K + kBlock - 1) / kBlock) * 4096 : 0) + (splits > 1 ? 16 * (size_t)splits * M * N : 0);
 }
 
 int mpc_matvec4(mpc_ctx* c, mpc_cshare x, const uint8_t* w, const int32_t* scales, mpc_share z,
@@ -228,9 +261,12 @@ int mpc_matvec4(mpc_ctx* c, mpc_cshare x, const uint8_t* w, const int32_t* scale
     if (!apart(z, out, w, (size_t)N * q.row_bytes) || !apart(z, out, scales, (size_t)N * q.groups * 4)) return MPC_EINVAL;
     q.w = w; q.scales = scales; q.M = M; q.K = K; q.N = N; q.group = group; q.shift = scale_bits;
     q.blocks = (K + kBlock - 1) / kBlock;
-    if (digits_in_memory(M, K, N)) {
-        if (!c->ws || c->ws_bytes < mpc_matvec4_workspace_bytes(M, K, N)) return MPC_ENOMEM;
-        q.digits = reinterpret_cast<uint32_t*>(c->ws);
+    q.splits = splits_of(M, K, N);
+    const size_t need = mpc_matvec4_workspace_bytes(M, K, N), partial = q.splits > 1 ? 16 * (size_t)q.splits * M * N : 0;
+    if (need) {
+        if (!c->ws || c->ws_bytes < need) return MPC_ENOMEM;
+        q.digits = reinterpret_cast<uint32_t*>(c->ws);                 // a multiple of 4 KB, if any
+        q.partial = reinterpret_cast<u64*>(reinterpret_cast<u8*>(c->ws) + (need - partial));
     }
     MPC_TRY(lane_first(c));
     if (group == 32) launch<32>(q, c->s[0]);

@@ -200,6 +200,21 @@ def test_matvec4_many_rows(mpc, lane, attention, M, K, N, group):
     equal(mpc, z, plain.matvec4(x, q, scales, group, 20))
 
 
+@pytest.mark.parametrize("M,K,N,group", [(1, 25088, 10, 32), (1, 16417, 100, 64), (2, 9000, 33, 128), (3, 8197, 40, 64), (9, 8200, 17, 256), (16, 25088, 400, 128)])
+def test_matvec4_columns_split_over_workgroups(mpc, attention, M, K, N, group):
+    """Long rows of few weights: the sums of several workgroups are joined, in a workspace of exactly the queried size."""
+    from test_gpu_workspace_bounds import Guarded
+    rng = np.random.default_rng(K + N)
+    need = mpc.lib().mpc_matvec4_workspace_bytes(M, K, N)
+    assert need >= 2 * 16 * M * N
+    g = Guarded(mpc, need)
+    g.lane._ws_bytes = need
+    x, q, s = inputs.masks(rng, M, K), rng.integers(-8, 8, (N, K)), rng.integers(-(1 << 31), 1 << 31, (N, -(-K // group))).astype(np.int32)
+    z = g.lane.matvec4(dev(mpc, x), attention.pack_weights4(torch.from_numpy(q)).cuda(), mpc.to_device(s), group, 16)
+    g.check()
+    equal(mpc, z, plain.matvec4(x, q, s, group, 16))
+
+
 def test_matvec4_extreme_weights(mpc, lane, attention):
     """Every weight -8, every scale -2^31 and words whose digits are all -128: the largest sums there are."""
     M, K, N = 2, 20000, 3
