@@ -30,9 +30,11 @@ constexpr int most_waves(int mt) { return mt == 1 ? 16 : 8; }
 
 // Whether the digits of x are made once, by a launch of their own, instead of by every workgroup for itself.  us with and without:
 // 8 x 25088 x 4096 51 / 76, 16 x 4096 x 4096 33 / 44; but 4 x 4096 x 4096 12 / 12, 8 x 1024 x 4096 13 / 11, 1 x 768 x 2304 7 / 4.
-bool digits_in_memory(int M, int K, int N) { return M > 4 && (long long)M * K * N >= 1ll << 27; }
+bool small(int M, int K, int N) { return (long long)M * K * N < 1ll << 27; }
+bool digits_in_memory(int M, int K, int N) { return M > 4 && !small(M, K, N); }
 
-// Rows of x to a workgroup.
+// Rows of x to a workgroup; launch() takes two of four where that is faster, us with four and two: 16 x 768 x 2304 12 / 10,
+// 4 x 768 x 768 6.7 / 4.8, but for larger products 4 x 25088 x 4096 40 / 43 and for groups of 32 4 x 4096 x 4096 15 / 20.
 int rows_at_once(int M, int K, int N) { return digits_in_memory(M, K, N) ? 8 : M < 3 ? M : 4; }
 // Into how many workgroups the columns are split: few rows of the weights that are long leave most units idle, and a workgroup's
 // waves go through several blocks one after the other.  The sums are added by a launch of their own.  us without and with:
@@ -228,7 +230,7 @@ template <int G> void launch(const MatvecArgs& q, hipStream_t st)
         launch<G, 8, true>(q, st);
     }
     else if (q.M == 1) launch<G, 1, false>(q, st);
-    else if (q.M == 2) launch<G, 2, false>(q, st);
+    else if (q.M == 2 || (G > 32 && small(q.M, q.K, q.N))) launch<G, 2, false>(q, st);
     else launch<G, 4, false>(q, st);
 }
 
