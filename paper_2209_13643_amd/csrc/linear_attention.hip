@@ -38,6 +38,7 @@ struct ChunkArgs {
     u64* box;
     int B, H, T, dk, dv, chunks, bits;
     int mt, nt;                               // tiles of 64 along dk and dv
+    int rows_jobs;                            // jobs that form P and W: one for all of W V, or one for each tile of dv
     unsigned cells;                           // chunks of all heads
 };
 
@@ -279,8 +280,7 @@ __global__ __launch_bounds__(kThreads) void k_chunk_open(ChunkArgs q)
     const Place at_start = place();
     const bool left = at_start.wave < 4;
     const Box box(q.box);
-    const auto to_box = [&](const Quad& e1, const Quad& e0) { box.put(e1, e0); };
-    for (Jobs job(q.cells, 1 + q.mt * q.nt); job.cell() < q.cells; job.next()) {
+    for (Jobs job(q.cells, q.rows_jobs + q.mt * q.nt); job.cell() < q.cells; job.next()) {
         const Place p = anew(at_start);
         const int kind = job.kind(), bh = job.cell() / q.chunks, chunk = job.cell() - bh * q.chunks;
         const int b = bh / q.H, h = bh - b * q.H, t0 = chunk * kChunk, L = min(q.T - t0, kChunk);
@@ -288,7 +288,9 @@ __global__ __launch_bounds__(kThreads) void k_chunk_open(ChunkArgs q)
         const long long at = (long long)bh * q.T + t0;            // the chunk's first token in the dense arrays
         const long long ok = b * q.k.b + h * q.k.h + t0 * q.k.t, ov = b * q.v.b + h * q.v.h + t0 * q.v.t;
         u64 z0[8], z1[8];                                         // start from the addends, asked for first
-        if (kind == 0) {
+        if (kind < q.rows_jobs) {
+            const int n_first = kind * 64, n_end = q.rows_jobs > 1 ? min(q.dv, n_first + 64) : q.dv;
+            const auto to_box = [&](const Quad& e1, const Quad& e0) { if (n_first == 0) box.put(e1, e0); };     // sent once
             // P turned round, K Q^T: a thread's four words of a column are neighbours in a row of W, a quad of the next product
             const int turned = p.wave % 4 * 16 + p.lane / 16 * 4, i0 = p.wave / 4 * 32 + p.lane % 16;    // j of its first word, i of tile 0
             const auto quad_at = [&](const u64* w, int t) {       // of [token][64]
@@ -325,9 +327,9 @@ __global__ __launch_bounds__(kThreads) void k_chunk_open(ChunkArgs q)
                     e0.w[j] = below ? w0 - a0.w[j] : 0; e1.w[j] = below ? w1 - a1.w[j] : 0;
                     own[t].w[j] = below ? w0 + e1.w[j] : 0; open[t].w[j] = e0.w[j] + e1.w[j]; mask[t].w[j] = below ? a1.w[j] : 0;
                 }
-                box.put(e1, e0);
+                to_box(e1, e0);
             }
-            for (int n0 = 0; n0 < q.dv; n0 += 64) {
+            for (int n0 = n_first; n0 < n_end; n0 += 64) {
                 const Place ps = anew(p);
                 const Tile<false, false> tv(ps, q.dv - n0, L);
                 const long long oa = at * q.dv + n0, o = ov + n0;
@@ -359,7 +361,7 @@ __global__ __launch_bounds__(kThreads) void k_chunk_open(ChunkArgs q)
                 });
             }
         } else {
-            const int m0 = (kind - 1) / q.nt * 64, n0 = (kind - 1) % q.nt * 64;      // contraction over the chunk's tokens
+            const int tile = kind - q.rows_jobs, m0 = tile / q.nt * 64, n0 = tile % q.nt * 64;      // contraction over the chunk's tokens
             const long long cell = (long long)job.cell() * q.dk * q.dv;
             each_word(p, [&](int r, int i, int j) {
                 const unsigned o = min(m0 + i, q.dk - 1) * q.dv + min(n0 + j, q.dv - 1);
@@ -676,8 +678,11 @@ int mpc_linear_attention(mpc_ctx* c, const mpc_attention_operands* x, const mpc_
     a.mt = (dk + 63) / 64; a.nt = (dv + 63) / 64; a.cells = (unsigned)((long long)B * H * p.chunks);
     const auto grid = [](long long jobs, long long most) { return dim3((unsigned)(jobs < most ? jobs : most)); };
     const long long rounds = (a.cells + 7) / 8 * 8;               // the same for every die
+    // With units to spare, P is formed again for each tile of W V: 8 heads of 128 x 128 over 200 tokens 83 -> 74 us.  In more than one round
+    // of workgroups that is work for nothing.
+    a.rows_jobs = rounds * (a.nt + a.mt * a.nt) <= kBoxes ? a.nt : 1;
     MPC_TRY(lane_first(c));
-    k_chunk_open<<<grid(rounds * (1 + a.mt * a.nt), kBoxes), kThreads, kOperands * kOperand, c->s[0]>>>(a);
+    k_chunk_open<<<grid(rounds * (a.rows_jobs + a.mt * a.nt), kBoxes), kThreads, kOperands * kOperand, c->s[0]>>>(a);
     k_chunk_states<<<grid(((long long)n_s / 8 + 255) / 256, kStateBoxes), 256, 0, c->s[0]>>>(a);
     k_chunk_out<<<grid(rounds * a.nt, kBoxes), kThreads, kOperands * kOperand, c->s[0]>>>(a);
     MPC_HIP(c, hipGetLastError());
