@@ -273,7 +273,7 @@ def test_step_on_any_words(mpc, lane, seed):
 
 PROMPT = [(1, 1, 1, 1, 1), (1, 2, 2, 5, 3), (2, 63, 1, 16, 16), (1, 64, 2, 64, 64), (1, 65, 1, 64, 64), (2, 130, 2, 48, 40), (1, 200, 1, 33, 70), (1, 128, 1, 128, 128),
           (1, 100, 1, 100, 65), (1, 320, 1, 64, 64), (3, 7, 3, 17, 15), (1, 90, 1, 65, 127),
-          (5, 100, 5, 70, 72)]                               # one job for all of W V, two tiles
+          (9, 100, 3, 70, 72)]                               # one job for all of W V, two tiles
 
 
 @pytest.mark.parametrize("state", [True, False])
