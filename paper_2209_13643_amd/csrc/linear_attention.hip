@@ -293,8 +293,9 @@ __global__ __launch_bounds__(kThreads) void k_chunk_open(ChunkArgs q)
             const auto to_box = [&](const Quad& e1, const Quad& e0) { if (n_first == 0) box.put(e1, e0); };     // sent once
             // P turned round, K Q^T: a thread's four words of a column are neighbours in a row of W, a quad of the next product
             const int turned = p.wave % 4 * 16 + p.lane / 16 * 4, i0 = p.wave / 4 * 32 + p.lane % 16;    // j of its first word, i of tile 0
-            const auto quad_at = [&](const u64* w, int t) {       // of [token][64]
-                const u64* const from = w + at * kChunk + (unsigned)(min(i0 + t * 16, L - 1) * kChunk + turned);
+            const auto quad_at = [&](const u64* w, int t) {       // of [token][64]; above the diagonal the row's last one again
+                const int i = min(i0 + t * 16, L - 1);
+                const u64* const from = w + at * kChunk + (unsigned)(i * kChunk + min(turned, i & ~3));
                 const u64x2u lo = *reinterpret_cast<const u64x2u*>(from), hi = *reinterpret_cast<const u64x2u*>(from + 2);
                 return Quad{ { lo.x, lo.y, hi.x, hi.y } };
             };
