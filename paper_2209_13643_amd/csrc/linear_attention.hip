@@ -271,8 +271,8 @@ struct Jobs {
 
 struct NoPower { __device__ uint32_t operator()(int, int) const { return 1; } };
 
-// P, W and W V of a chunk, or one tile of its U.  8 x 512 tokens of 12 heads of 64 x 64: 218 us of the call's 296, 0.76 GB.  Bound by
-// what follows one another in a product: its loads (3.5 TB/s over all), the digits (vector instructions fill 23 % of the cycles)
+// P, W and W V of a chunk, or one tile of its U.  8 x 512 tokens of 12 heads of 64 x 64: 218 us of the call's 294, 0.71 GB.  Bound by
+// what follows one another in a product: its loads (3.3 TB/s over all), the digits (vector instructions fill 23 % of the cycles)
 // and the matrix instructions (14 %), since five operand tiles leave room for one workgroup to a compute unit.
 __global__ __launch_bounds__(kThreads) void k_chunk_open(ChunkArgs q)
 {

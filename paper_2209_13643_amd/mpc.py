@@ -977,7 +977,6 @@ class Lane:
         self._check(fn(self._h, _share(x), byref(m1), byref(m2), _share(y), B, H, W, C, n_chunks))
         return y
 
-    # -- dealer helpers (offline phase stand-in)
     # -- attention without a softmax, public 4-bit weights
     def position_bias(self, scores, table, buckets, out=None):
         """scores [B, H, Tq, Tk] + table [n, H] at the public bucket of every pair: buckets int32 [Tq + Tk - 1], entry
@@ -1099,6 +1098,7 @@ class Lane:
                     L.mpc_linear_attention_step(self._h, x, _pack_step(*at[n_x:]), *lead, dk, dv))
         return out, state_out
 
+    # -- dealer helpers (offline phase stand-in)
     def ring_matmul(self, L, R):
         shp = L.shape
         batch = 1 if len(shp) == 2 else shp[0]
