@@ -162,6 +162,32 @@ def test_position_bias_beyond_32_bit_offsets(mpc, lane, attention):
             assert torch.equal(grad[p][:, h], want)
 
 
+@pytest.mark.parametrize("B,H,T,n,causal", [(1, 2, 1175, 32, True), (1, 1, 6000, 300, False), (2, 3, 1100, 257, True), (5, 2, 1030, 7, False)])
+def test_position_bias_shared_out(mpc, lane, attention, B, H, T, n, causal):
+    """Several shares of the diagonals, several items to a workgroup: table and scores against sums of int64 tensors."""
+    g = torch.Generator(device="cuda:0").manual_seed(T)
+    x = tuple(torch.randint(-2 ** 63, 2 ** 63 - 1, (B, H, T, T), generator=g, device="cuda:0") for _ in range(2))
+    t = tuple(torch.randint(-2 ** 63, 2 ** 63 - 1, (n, H), generator=g, device="cuda:0") for _ in range(2))
+    m = torch.randint(-1, n, (2 * T - 1,), generator=g, device="cuda:0", dtype=torch.int32)
+    if causal:
+        m[T:] = -1                                           # entry j - i + T - 1
+    torch.cuda.synchronize()
+    y, gx = lane.position_bias(x, t, m), tuple(torch.empty_like(w) for w in x)
+    only, _ = lane.position_bias_grad(x, m, n)
+    both, _ = lane.position_bias_grad(x, m, n, scores_out=gx)
+    lane.sync()
+    i = torch.arange(T, device="cuda:0")
+    at = m.long()[i - i[:, None] + T - 1]
+    kept, at = at >= 0, at.clamp(min=0)
+    for p in range(2):
+        assert torch.equal(gx[p], x[p] * kept)
+        for h in range(H):
+            assert torch.equal(y[p][:, h], (x[p][:, h] + t[p][at, h]) * kept)
+            want = torch.zeros(n, dtype=torch.int64, device="cuda:0")
+            want.index_add_(0, at.flatten(), (x[p][:, h].sum(0) * kept).flatten())
+            assert torch.equal(only[p][:, h], want) and torch.equal(both[p][:, h], want)
+
+
 # ------------------------------------------------------------------------------------------------ 4-bit weights
 @pytest.mark.parametrize("M,K,N,group", [(1, 1, 1, 32), (1, 32, 16, 32), (2, 33, 5, 32), (1, 64, 17, 64), (3, 100, 40, 64), (1, 127, 15, 128), (4, 129, 33, 128),
                                          (1, 700, 64, 128), (5, 1000, 50, 32), (8, 513, 31, 64), (9, 300, 20, 256), (17, 96, 70, 32), (1, 2500, 130, 32),
@@ -213,6 +239,32 @@ def test_matvec4_columns_split_over_workgroups(mpc, attention, M, K, N, group):
     z = g.lane.matvec4(dev(mpc, x), attention.pack_weights4(torch.from_numpy(q)).cuda(), mpc.to_device(s), group, 16)
     g.check()
     equal(mpc, z, plain.matvec4(x, q, s, group, 16))
+
+
+def test_matvec4_recorded(mpc, attention):
+    """One graph of products that take a workspace (digits in memory, columns split, both): replays with eager work between."""
+    rng, ln, calls = np.random.default_rng(8), mpc.Lane(0, single_queue=True), []
+    for M, K, N, group in [(8, 4097, 4100, 64), (1, 16417, 40, 32), (16, 25088, 400, 128)]:
+        q, s = rng.integers(-8, 8, (N, K)), rng.integers(-(1 << 31), 1 << 31, (N, -(-K // group))).astype(np.int32)
+        calls.append((dev(mpc, inputs.masks(rng, M, K)), attention.pack_weights4(torch.from_numpy(q)).cuda(), mpc.to_device(s), group, filled((M, N)), q, s))
+    def run():
+        for x, w, s, group, z, _, _ in calls:
+            ln.matvec4(x, w, s, group, 16, out=z)
+    torch.cuda.synchronize()
+    run(); ln.sync()
+    with ln.capture() as cap:
+        run()
+    for _ in range(3):
+        for x, *_, q, s in calls:                            # other words for every replay
+            for t in x:
+                t.add_(t << 7)
+        torch.cuda.synchronize()
+        cap.graph.launch(ln)
+        ln.sync()
+        for x, w, _, group, z, q, s in calls:
+            equal(mpc, z, plain.matvec4(tuple(mpc.to_host(t) for t in x), q, s, group, 16))
+    cap.graph.close()
+    ln.close()
 
 
 def test_matvec4_extreme_weights(mpc, lane, attention):
