@@ -18,6 +18,7 @@ constexpr int kTilePairs = 4096;         // (i, j) pairs of a tile, at most
 
 constexpr int kAtOnce = 8;               // rows of the gradient on their way at a time
 constexpr size_t kEnough = 2048;         // workgroups; of the gradient up to four times as many
+constexpr size_t kFewRounds = 8;
 constexpr int kFewBuckets = 256;         // with more, a workgroup's partial sums cost too much for that
 constexpr unsigned kMostWaves = 8;       // of them
 
@@ -74,7 +75,7 @@ __global__ __launch_bounds__(kThreads) void k_position_bias(BiasArgs q)
 
 // A wave takes 128 diagonals of a block of rows, two to a lane, through all matrices of its workgroup, and keeps their sums in
 // registers: a row's words are read side by side, and one sum a diagonal goes to its bucket in LDS; the workgroups' buckets are added
-// up by a second launch (atomics on the table would need a launch ahead to clear it).  Diagonal k of a block of `rows` rows
+// up by a second launch unless there is one to a head (atomics on the table would need a launch ahead to clear it).  Diagonal k of a block of `rows` rows
 // from i0 on holds the pairs (i0 + r, r + k - (rows - 1)).  Row blocks follow one another: shares of diagonals that do not read
 // (masked ones) and those that do would otherwise go to different dies (18 x 1121 x 1121, causal: 162 us, so 135).
 // 96 x 512 x 512: 77 us with the sums' launch, 5.2 TB/s.
@@ -142,7 +143,8 @@ __global__ __launch_bounds__(64 * kMostWaves) void k_position_bias_grad(BiasArgs
     }
     __syncthreads();
     for (int u = threadIdx.x; u < q.n_buckets; u += blockDim.x)
-        q.partial[((size_t)(party * q.H + h) * q.n_buckets + u) * q.parts + part] = sums[u];
+        if (q.parts == 1) q.grad[party][(size_t)u * q.H + h] = sums[u];
+        else q.partial[((size_t)(party * q.H + h) * q.n_buckets + u) * q.parts + part] = sums[u];
 }
 
 // the workgroups' sums of a bucket and head, a wave each
@@ -171,6 +173,9 @@ void share_out(BiasArgs& q)
         const unsigned waves = (unsigned)((diagonals + 127) / 128);
         q.row_tiles = (q.Tq + q.rows - 1) / q.rows; q.col_tiles = (waves + kMostWaves - 1) / kMostWaves;
         q.waves = (waves + q.col_tiles - 1) / q.col_tiles;
+        // A party's head that is a few rounds of loads is one workgroup's, which then needs no second launch: 12 x 64 x 64 11.5 us a call
+        // with two, 9.8 with one (of the device 6.5 and 7.2), 24 x 1 x 115 11.7 and 10.4 (5.2 and 4.4).
+        if ((size_t)q.B * q.row_tiles * q.col_tiles * ((q.rows + kAtOnce - 1) / kAtOnce) <= kFewRounds) { q.batches = q.B; q.splits = q.parts = 1; return; }
         one = 2 * (size_t)q.H * q.row_tiles * q.col_tiles;
         if (one * q.B >= kEnough || q.rows <= 8) break;
     }
@@ -250,7 +255,7 @@ int mpc_position_bias_grad(mpc_ctx* c, mpc_cshare g, const int32_t* buckets, mpc
     const size_t lds = (size_t)n_buckets * 8;
     if (scores) k_position_bias_grad<true><<<grid, block, lds, c->s[0]>>>(q);
     else k_position_bias_grad<false><<<grid, block, lds, c->s[0]>>>(q);
-    k_position_bias_sums<<<dim3((unsigned)sums), kSumThreads, 0, c->s[0]>>>(q);
+    if (q.parts > 1) k_position_bias_sums<<<dim3((unsigned)sums), kSumThreads, 0, c->s[0]>>>(q);
     MPC_HIP(c, hipGetLastError());
     return lane_fanout(c);
 }
