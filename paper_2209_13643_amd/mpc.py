@@ -24,6 +24,7 @@ MPC_TRANS_X = 4
 MPC_TRANS_Y = 8
 MPC_FOLDED = 16
 MPC_TWO_PHASE = 2
+MPC_ENOMEM = -2
 PROF_GEMM_KERNEL, PROF_LINEAR, PROF_RELU = 0, 1, 2
 N_AND_TRIPLES = 12
 
@@ -978,6 +979,14 @@ class Lane:
         return y
 
     # -- attention without a softmax, public 4-bit weights
+    def _call(self, entry, query, size, *args):
+        """An entry point that takes a workspace; asked for its size only where the lane's does not do (nothing is enqueued then)."""
+        rc = entry(*args)
+        if rc == MPC_ENOMEM:
+            self.reserve(query(*size))
+            rc = entry(*args)
+        self._check(rc)
+
     def position_bias(self, scores, table, buckets, out=None):
         """scores [B, H, Tq, Tk] + table [n, H] at the public bucket of every pair: buckets int32 [Tq + Tk - 1], entry
         j - i + Tq - 1 of query i and key j; an entry outside [0, n) masks its pairs (zero).  out may be scores."""
@@ -1003,14 +1012,11 @@ class Lane:
         ts, small = _pairs(("g", g), ("out", out), ("scores_out", scores_out if scores_out is not None else g)), (n_buckets, H)
         at = _words(ts, [shape, shape, small, small, shape, shape], self._index, ("g", "out", "scores_out"))
         m = _dense(buckets, (Tq + Tk - 1,), torch.int32, self._index, "buckets")
-        L = lib()
-        need = L.mpc_position_bias_grad_workspace_bytes(B, H, Tq, Tk, n_buckets)
-        if need == 0 or need > self._ws_bytes:
-            self.reserve(need)
         ts.append(buckets)
         self._pending += ts
-        self._check(L.mpc_position_bias_grad(self._h, _share_at(at, 0), m, _share_at(at, 2), _share_at(at, 4) if scores_out is not None else CShare(),
-                                             B, H, Tq, Tk, n_buckets))
+        L = lib()
+        self._call(L.mpc_position_bias_grad, L.mpc_position_bias_grad_workspace_bytes, (B, H, Tq, Tk, n_buckets),
+                   self._h, _share_at(at, 0), m, _share_at(at, 2), _share_at(at, 4) if scores_out is not None else CShare(), B, H, Tq, Tk, n_buckets)
         return out, scores_out
 
     def matvec4(self, x, w, scales, group, scale_bits=16, out=None):
@@ -1026,13 +1032,10 @@ class Lane:
         at = _words(ts, [shape, shape, result, result], self._index, ("x", "out"))
         wp = _dense(w, (N, (K + 31) // 32 * 16), torch.uint8, self._index, "w")
         sp = _dense(scales, (N, -(-K // group)), torch.int32, self._index, "scales")
-        L = lib()
-        need = L.mpc_matvec4_workspace_bytes(M, K, N)
-        if need > self._ws_bytes:
-            self.reserve(need)
         ts += (w, scales)
         self._pending += ts
-        self._check(L.mpc_matvec4(self._h, _share_at(at, 0), wp, sp, _share_at(at, 2), M, K, N, group, scale_bits))
+        L = lib()
+        self._call(L.mpc_matvec4, L.mpc_matvec4_workspace_bytes, (M, K, N), self._h, _share_at(at, 0), wp, sp, _share_at(at, 2), M, K, N, group, scale_bits)
         return out
 
     def linear_attention(self, q, k, v, decay, mat, state=None, out=None, state_out=None):
@@ -1086,16 +1089,16 @@ class Lane:
                     "and with the same strides for both shares, the others dense, the material by its number of words,")
         at = list(map(_ptr, ts))
         d = _dense(decay, (H, ATTENTION_CHUNK + 1), torch.int32, index, "decay")
-        need = (L.mpc_linear_attention_workspace_bytes if prompt else L.mpc_linear_attention_step_workspace_bytes)(*lead, dk, dv)
-        if need == 0 or need > self._ws_bytes:
-            self.reserve(need)
         ts.append(decay)
         self._pending += ts
         sq, sk, sv, so = strides[0::2]
         sq, sk, sv, so = (sq[:3], sk[:3], sv[:3], so[:3]) if prompt else ((sq[0], 0, sq[1]), (sk[0], 0, sk[1]), (sv[0], 0, sv[1]), (so[0], 0, so[1]))
         x = _pack_operands(*at[:6], *sq, *sk, *sv, d, *(at[10:12] if state is not None else (0, 0)), at[6], at[7], *so, at[8], at[9])
-        self._check(L.mpc_linear_attention(self._h, x, _pack_prompt(*at[n_x:]), *lead, dk, dv) if prompt else
-                    L.mpc_linear_attention_step(self._h, x, _pack_step(*at[n_x:]), *lead, dk, dv))
+        size = (*lead, dk, dv)
+        if prompt:
+            self._call(L.mpc_linear_attention, L.mpc_linear_attention_workspace_bytes, size, self._h, x, _pack_prompt(*at[n_x:]), *size)
+        else:
+            self._call(L.mpc_linear_attention_step, L.mpc_linear_attention_step_workspace_bytes, size, self._h, x, _pack_step(*at[n_x:]), *size)
         return out, state_out
 
     # -- dealer helpers (offline phase stand-in)
