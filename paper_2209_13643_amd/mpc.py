@@ -979,12 +979,14 @@ class Lane:
         return y
 
     # -- attention without a softmax, public 4-bit weights
-    def _call(self, entry, query, size, *args):
-        """An entry point that takes a workspace; asked for its size only where the lane's does not do (nothing is enqueued then)."""
+    def _call(self, tensors, entry, query, size, *args):
+        """An entry point that takes a workspace; asked for its size only where the lane's does not do (nothing is enqueued then).
+        The call's tensors are noted behind that: a workspace that grows waits for the lane, which lets go of all noted before."""
         rc = entry(*args)
         if rc == MPC_ENOMEM:
             self.reserve(query(*size))
             rc = entry(*args)
+        self._pending += tensors
         self._check(rc)
 
     def position_bias(self, scores, table, buckets, out=None):
@@ -1013,9 +1015,8 @@ class Lane:
         at = _words(ts, [shape, shape, small, small, shape, shape], self._index, ("g", "out", "scores_out"))
         m = _dense(buckets, (Tq + Tk - 1,), torch.int32, self._index, "buckets")
         ts.append(buckets)
-        self._pending += ts
         L = lib()
-        self._call(L.mpc_position_bias_grad, L.mpc_position_bias_grad_workspace_bytes, (B, H, Tq, Tk, n_buckets),
+        self._call(ts, L.mpc_position_bias_grad, L.mpc_position_bias_grad_workspace_bytes, (B, H, Tq, Tk, n_buckets),
                    self._h, _share_at(at, 0), m, _share_at(at, 2), _share_at(at, 4) if scores_out is not None else CShare(), B, H, Tq, Tk, n_buckets)
         return out, scores_out
 
@@ -1033,9 +1034,8 @@ class Lane:
         wp = _dense(w, (N, (K + 31) // 32 * 16), torch.uint8, self._index, "w")
         sp = _dense(scales, (N, -(-K // group)), torch.int32, self._index, "scales")
         ts += (w, scales)
-        self._pending += ts
         L = lib()
-        self._call(L.mpc_matvec4, L.mpc_matvec4_workspace_bytes, (M, K, N), self._h, _share_at(at, 0), wp, sp, _share_at(at, 2), M, K, N, group, scale_bits)
+        self._call(ts, L.mpc_matvec4, L.mpc_matvec4_workspace_bytes, (M, K, N), self._h, _share_at(at, 0), wp, sp, _share_at(at, 2), M, K, N, group, scale_bits)
         return out
 
     def linear_attention(self, q, k, v, decay, mat, state=None, out=None, state_out=None):
@@ -1090,15 +1090,14 @@ class Lane:
         at = list(map(_ptr, ts))
         d = _dense(decay, (H, ATTENTION_CHUNK + 1), torch.int32, index, "decay")
         ts.append(decay)
-        self._pending += ts
         sq, sk, sv, so = strides[0::2]
         sq, sk, sv, so = (sq[:3], sk[:3], sv[:3], so[:3]) if prompt else ((sq[0], 0, sq[1]), (sk[0], 0, sk[1]), (sv[0], 0, sv[1]), (so[0], 0, so[1]))
         x = _pack_operands(*at[:6], *sq, *sk, *sv, d, *(at[10:12] if state is not None else (0, 0)), at[6], at[7], *so, at[8], at[9])
         size = (*lead, dk, dv)
         if prompt:
-            self._call(L.mpc_linear_attention, L.mpc_linear_attention_workspace_bytes, size, self._h, x, _pack_prompt(*at[n_x:]), *size)
+            self._call(ts, L.mpc_linear_attention, L.mpc_linear_attention_workspace_bytes, size, self._h, x, _pack_prompt(*at[n_x:]), *size)
         else:
-            self._call(L.mpc_linear_attention_step, L.mpc_linear_attention_step_workspace_bytes, size, self._h, x, _pack_step(*at[n_x:]), *size)
+            self._call(ts, L.mpc_linear_attention_step, L.mpc_linear_attention_step_workspace_bytes, size, self._h, x, _pack_step(*at[n_x:]), *size)
         return out, state_out
 
     # -- dealer helpers (offline phase stand-in)
