@@ -254,7 +254,7 @@ int mpc_matvec4(mpc_ctx* c, mpc_cshare x, const uint8_t* w, const int32_t* scale
     for (int i = 0; i < 2; ++i) if (!x.p[i] || !z.p[i]) return MPC_EINVAL;
     if (K > MPC_MAX_K_TOTAL || M > 65535 || N > kMostN) return MPC_ERANGE;
     MatvecArgs q{};
-    q.groups = (K + group - 1) / group; q.row_bytes = (K + 31) / 32 * 16;
+    q.groups = K / group + (K % group != 0); q.row_bytes = (K + 31) / 32 * 16;
     const size_t out = (size_t)M * N * 8;
     if (!outputs_apart(z, out, x, (size_t)M * K * 8, false)) return MPC_EINVAL;
     for (int i = 0; i < 2; ++i) {
