@@ -531,9 +531,10 @@ int mpc_maxpool2x2_backward(mpc_ctx* ctx, mpc_cshare g, mpc_cshare s1, mpc_cshar
  * mpc_position_bias_grad: table_grad[u][h] = sum of g[b][h][i][j] over b and all pairs of bucket u (written, not added to);
  * scores_grad (both NULL to skip; may be g itself) = g, zero at masked pairs.  Sums mod 2^64 are exact: the result does not
  * depend on their order.  Workspace: the query.
- * MPC_ERANGE: n_buckets > MPC_MAX_BUCKETS, Tq + Tk, B * H or 2 * H * n_buckets near 2^31, more than 2^22 tiles (of 4096 pairs at most,
- * each within a matrix) or, for the gradient, 2^25 entries of the table. */
+ * MPC_ERANGE: n_buckets > MPC_MAX_BUCKETS, Tq + Tk, B * H or 2 * H * n_buckets near 2^31, more than MPC_MAX_PAIRS pairs, more than
+ * 2^22 tiles (of 4096 pairs at most, each within a matrix) or, for the gradient, 2^25 entries of the table. */
 #define MPC_MAX_BUCKETS 4096
+#define MPC_MAX_PAIRS (1ll << 40)                  /* B * H * Tq * Tk */
 int mpc_position_bias(mpc_ctx* ctx, mpc_cshare scores, mpc_cshare table, const int32_t* buckets, mpc_share out,
                       int B, int H, int Tq, int Tk, int n_buckets);
 size_t mpc_position_bias_grad_workspace_bytes(int B, int H, int Tq, int Tk, int n_buckets);

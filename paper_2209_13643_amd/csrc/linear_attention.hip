@@ -605,7 +605,8 @@ int shape_ok(mpc_ctx* c, int B, int T, int H, int dk, int dv)
 {
     if (B <= 0 || T <= 0 || H <= 0 || dk <= 0 || dv <= 0) return MPC_EINVAL;
     if (dk > MPC_ATTENTION_MAX_D || dv > MPC_ATTENTION_MAX_D || H > INT32_MAX / (kChunk + 1) || T > INT32_MAX - kChunk) return MPC_ERANGE;
-    if (((long long)T + kChunk - 1) / kChunk * B * H > INT32_MAX / 5) return MPC_ERANGE;      // jobs of a launch
+    const long long chunks = (T + kChunk - 1) / kChunk, heads = (long long)B * H;
+    if (heads > INT32_MAX / 5 || chunks > INT32_MAX / 5 / heads) return MPC_ERANGE;           // jobs of a launch; no product past 64 bits
     return c && c->frac_bits > 30 ? MPC_ERANGE : MPC_OK;       // a decay of one has to fit 31 bits
 }
 

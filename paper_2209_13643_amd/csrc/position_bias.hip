@@ -192,6 +192,7 @@ int bias_shape(BiasArgs& q, int B, int H, int Tq, int Tk, int n_buckets)
     if (B <= 0 || H <= 0 || Tq <= 0 || Tk <= 0 || n_buckets <= 0) return MPC_EINVAL;
     if (n_buckets > MPC_MAX_BUCKETS || (long long)Tq + Tk > INT32_MAX - 2048 ||      // diagonals are counted in int, up to 1024 of a workgroup at a time
         (long long)B * H > INT32_MAX || 2ll * H * n_buckets > INT32_MAX) return MPC_ERANGE;
+    if ((long long)Tq * Tk > MPC_MAX_PAIRS / ((long long)B * H)) return MPC_ERANGE;      // by division: bytes and tiles are counted in 64 bits
     q.B = B; q.H = H; q.BH = (unsigned)B * H; q.Tq = Tq; q.Tk = Tk; q.n_buckets = n_buckets;
     return MPC_OK;
 }

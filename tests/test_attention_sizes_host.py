@@ -29,3 +29,28 @@ def test_groups_beyond_an_int_are_refused(library, group):  # noqa: F811
     with pytest.raises(ValueError):
         host_lane().matvec4(pair(1, 64), torch.zeros(3, 32, dtype=torch.uint8), torch.ones(3, 1, dtype=torch.int32), group)
     assert not library.calls
+
+
+WRAPPED = r'''
+lib.mpc_linear_attention_workspace_bytes.restype = lib.mpc_linear_attention_step_workspace_bytes.restype = c_size_t
+lib.mpc_ctx_set_workspace(ctx, array(big), big)
+# products of the sizes that are 2^64, so zero in 64 bits, or come out small
+result["queries"] = [lib.mpc_linear_attention_workspace_bytes(1 << 30, 1 << 30, 1 << 10, 8, 8), lib.mpc_linear_attention_workspace_bytes(1 << 25, 1 << 30, 1 << 15, 8, 8),
+                     lib.mpc_position_bias_grad_workspace_bytes(1 << 20, 1 << 10, 1 << 30, 1 << 30, 4)]
+sizes = [dict(B=1 << 30, H=1, Tq=1 << 15, Tk=1 << 30), dict(B=1 << 20, H=1 << 10, Tq=1 << 15, Tk=1 << 30), dict(B=1, H=1, Tq=1 << 30, Tk=(1 << 30) - 4096)]
+result["bias"] = [bias(**s) for s in sizes]
+result["grad"] = [grad(**s) for s in sizes]
+def prompts(**s):
+    lib.mpc_ctx_set_workspace(ctx, array(big), 1 << 30)
+    mat = Material((Share * 10)(*[share(big) for i in range(10)]))
+    x = Operands(share(big), share(big), share(big), Strides(), Strides(), Strides(), array(big), none, share(big), Strides(1 << 40, 8, 8), none)
+    return lib.mpc_linear_attention(ctx, ctypes.byref(x), ctypes.byref(mat), s["B"], s["T"], s["H"], 8, 8)
+result["prompt"] = [prompts(B=1 << 30, T=1 << 30, H=1 << 10), prompts(B=1 << 25, T=1 << 30, H=1 << 15)]
+result["launched"] = launches()
+'''
+
+
+def test_sizes_whose_product_wraps_are_refused(tmp_path):
+    r = fake_hip.run(tmp_path, REFUSALS + WRAPPED)
+    assert r["queries"] == [0, 0, 0] and r["bias"] == [R] * 3 and r["grad"] == [R] * 3 and r["prompt"] == [R] * 2
+    assert r["launched"] == []
