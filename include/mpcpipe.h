@@ -575,10 +575,12 @@ int mpc_matvec4(mpc_ctx* ctx, mpc_cshare x, const uint8_t* w, const int32_t* sca
  *     c_p [BH][T][64] of a_q a_k^T, c_u [BH][chunks][dk][dv] of a_kd^T a_v, c_o [BH][T][dv] of a_w a_v + a_qd a_s
  *   step: a_q, a_k [BH][dk], a_v [BH][dv], a_s [BH][dk][dv] (mask of S'); c_u [BH][dk][dv] of a_k a_v^T, c_o [BH][dv] of a_q a_s
  * MPC_ERANGE: dk or dv beyond MPC_ATTENTION_MAX_D, frac_bits > 30, H beyond 2^31 / 65, B * H * chunks beyond 2^31 / 5, an input
- * token stride of a prompt beyond MPC_ATTENTION_MAX_TOKEN_STRIDE.  Workspace: the queries. */
+ * token stride of a prompt beyond MPC_ATTENTION_MAX_TOKEN_STRIDE, an axis of q, k, v or o whose last entry lies more than
+ * MPC_ATTENTION_MAX_EXTENT words behind its first.  Workspace: the queries. */
 #define MPC_ATTENTION_CHUNK 64
 #define MPC_ATTENTION_MAX_D 128
 #define MPC_ATTENTION_MAX_TOKEN_STRIDE 4194303     /* of q, k, v of a prompt, in words */
+#define MPC_ATTENTION_MAX_EXTENT (1ll << 40)       /* words */
 typedef struct { int64_t batch, token, head; } mpc_strides;
 typedef struct {
     mpc_cshare q, k, v;

@@ -572,6 +572,12 @@ __global__ __launch_bounds__(256, 4) void k_step(StepArgs q)
 
 bool strides_in(const mpc_strides& s) { return s.batch >= 0 && s.token >= 0 && s.head >= 0; }
 bool far_tokens(const mpc_strides& s) { return s.token > kMaxStride; }
+// beyond MPC_ATTENTION_MAX_EXTENT words from the first entry of an axis to its last one: offsets are counted in 64 bits
+bool far_apart(const mpc_strides& s, int B, int T, int H)
+{
+    const auto far = [](long long stride, int n) { return n > 1 && stride > MPC_ATTENTION_MAX_EXTENT / (n - 1); };
+    return far(s.batch, B) || far(s.token, T) || far(s.head, H);
+}
 
 // words from the first to the last one of [B][T][H][d] with these strides
 size_t extent(const mpc_strides& s, int B, int T, int H, int d)
@@ -582,7 +588,6 @@ size_t extent(const mpc_strides& s, int B, int T, int H, int d)
 // no two of the output's words share a place: in the order of their strides, every axis steps over the ones within it
 bool strides_out(const mpc_strides& s, int B, int T, int H, int d)
 {
-    if (!strides_in(s)) return false;
     long long st[3] = { s.batch, s.token, s.head }; int n[3] = { B, T, H };
     for (int i = 0; i < 2; ++i)
         for (int j = 0; j < 2 - i; ++j)
@@ -644,7 +649,9 @@ int mpc_linear_attention(mpc_ctx* c, const mpc_attention_operands* x, const mpc_
     const mpc_cshare* const mats[] = { &m->a_q, &m->a_k, &m->a_qd, &m->a_kd, &m->a_v, &m->a_w, &m->a_s, &m->c_p, &m->c_u, &m->c_o };
     for (const mpc_cshare* w : mats) if (!both(*w)) return MPC_EINVAL;
     MPC_TRY(shape_ok(c, B, T, H, dk, dv));
-    if (!strides_in(sq) || !strides_in(sk) || !strides_in(sv) || !strides_out(so, B, T, H, dv)) return MPC_EINVAL;
+    if (!strides_in(sq) || !strides_in(sk) || !strides_in(sv) || !strides_in(so)) return MPC_EINVAL;
+    if (far_apart(sq, B, T, H) || far_apart(sk, B, T, H) || far_apart(sv, B, T, H) || far_apart(so, B, T, H)) return MPC_ERANGE;
+    if (!strides_out(so, B, T, H, dv)) return MPC_EINVAL;
     if (far_tokens(sq) || far_tokens(sk) || far_tokens(sv)) return MPC_ERANGE;
     const ChunkPlan p = plan(B, T, H, dk, dv);
     const size_t n_o = extent(so, B, T, H, dv) * 8, n_s = (size_t)B * H * dk * dv * 8;
@@ -700,7 +707,9 @@ int mpc_linear_attention_step(mpc_ctx* c, const mpc_attention_operands* x, const
     for (const mpc_cshare* w : mats) if (!both(*w)) return MPC_EINVAL;
     MPC_TRY(shape_ok(c, B, 1, H, dk, dv));
     sq.token = sk.token = sv.token = so.token = 0;
-    if (!strides_in(sq) || !strides_in(sk) || !strides_in(sv) || !strides_out(so, B, 1, H, dv)) return MPC_EINVAL;
+    if (!strides_in(sq) || !strides_in(sk) || !strides_in(sv) || !strides_in(so)) return MPC_EINVAL;
+    if (far_apart(sq, B, 1, H) || far_apart(sk, B, 1, H) || far_apart(sv, B, 1, H) || far_apart(so, B, 1, H)) return MPC_ERANGE;
+    if (!strides_out(so, B, 1, H, dv)) return MPC_EINVAL;
     const size_t BH = (size_t)B * H * 8, n_s = BH * dk * dv, n_o = extent(so, B, 1, H, dv) * 8;
     const size_t sizes[] = { BH * dk, BH * dk, BH * dv, n_s, n_s, BH * dv };
     const mpc_cshare* const in[] = { &q, &k, &v };

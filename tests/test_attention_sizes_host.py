@@ -54,3 +54,21 @@ def test_sizes_whose_product_wraps_are_refused(tmp_path):
     r = fake_hip.run(tmp_path, REFUSALS + WRAPPED)
     assert r["queries"] == [0, 0, 0] and r["bias"] == [R] * 3 and r["grad"] == [R] * 3 and r["prompt"] == [R] * 2
     assert r["launched"] == []
+
+
+STRIDES = r'''
+far = 1 << 62                                                # four batches of it are 2^64 words
+o = share(big)
+result["prompt"] = [prompt(B=5, sq=Strides(far, H * dk, dk)), prompt(B=5, q=o, o=o, sq=Strides(far, H * dk, dk)), prompt(B=5, so=Strides(far, 18, 6)),
+                    prompt(B=2, sq=Strides((1 << 40) + 1, H * dk, dk)), prompt(T=3, so=Strides(18, 1 << 40, 6)), prompt(H=3, so=Strides(18, 6, (1 << 39) + 1))]
+result["step"] = [step(B=5, so=Strides(far, 0, 6)), step(H=5, so=Strides(30, 0, far))]
+result["launched by refused calls"] = launches()
+# an axis of one entry has no use for its stride
+result["one"] = [prompt(B=1, sq=Strides(far, H * dk, dk), so=Strides(far, 18, 6)), step(B=1, so=Strides(far, 0, 6))]
+'''
+
+
+def test_strides_whose_extent_wraps_are_refused(tmp_path):
+    r = fake_hip.run(tmp_path, REFUSALS + "launches()\n" + STRIDES)
+    assert r["prompt"] == [R] * 6 and r["step"] == [R] * 2 and r["launched by refused calls"] == []
+    assert r["one"] == [0] * 2
