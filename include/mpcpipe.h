@@ -556,7 +556,8 @@ int mpc_matvec4(mpc_ctx* ctx, mpc_cshare x, const uint8_t* w, const int32_t* sca
 /* Linear attention with a public decay g for each head: S_t = g S_(t-1) + k_t v_t^T (dk x dv), o_t = q_t S_t.
  *
  * Where the words of q, k, v, o lie: word e of (batch b, token t, head h) at b*batch + t*token + h*head + e, strides in
- * words, both shares alike; any non-negative strides for inputs, outputs without words that share a place.
+ * words, both shares alike; any non-negative strides for inputs, outputs without words that share a place.  The stride of an
+ * axis of one entry is not used.
  * decay: int32 [H][65] on the device, public: entry n of a head is rint(g^n * 2^frac_bits); every entry in [0, 2^31).
  * Everything else is dense.
  *

@@ -571,7 +571,7 @@ __global__ __launch_bounds__(256, 4) void k_step(StepArgs q)
 }
 
 bool strides_in(const mpc_strides& s) { return s.batch >= 0 && s.token >= 0 && s.head >= 0; }
-bool far_tokens(const mpc_strides& s) { return s.token > kMaxStride; }
+bool far_tokens(const mpc_strides& s, int T) { return T > 1 && s.token > kMaxStride; }
 // beyond MPC_ATTENTION_MAX_EXTENT words from the first entry of an axis to its last one: offsets are counted in 64 bits
 bool far_apart(const mpc_strides& s, int B, int T, int H)
 {
@@ -652,7 +652,7 @@ int mpc_linear_attention(mpc_ctx* c, const mpc_attention_operands* x, const mpc_
     if (!strides_in(sq) || !strides_in(sk) || !strides_in(sv) || !strides_in(so)) return MPC_EINVAL;
     if (far_apart(sq, B, T, H) || far_apart(sk, B, T, H) || far_apart(sv, B, T, H) || far_apart(so, B, T, H)) return MPC_ERANGE;
     if (!strides_out(so, B, T, H, dv)) return MPC_EINVAL;
-    if (far_tokens(sq) || far_tokens(sk) || far_tokens(sv)) return MPC_ERANGE;
+    if (far_tokens(sq, T) || far_tokens(sk, T) || far_tokens(sv, T)) return MPC_ERANGE;
     const ChunkPlan p = plan(B, T, H, dk, dv);
     const size_t n_o = extent(so, B, T, H, dv) * 8, n_s = (size_t)B * H * dk * dv * 8;
     const size_t BHT = (size_t)B * H * T * 8;

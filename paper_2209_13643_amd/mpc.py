@@ -1091,6 +1091,8 @@ class Lane:
         shapes = [row, row, row, row, col, col, col, col, cell, cell, cell, cell][:n_x]
         numbers = list(map(_numel, ts[n_x:]))
         strides = list(map(_stride, ts[:8]))
+        if strides[0::2] != strides[1::2]:                   # the stride of an axis of one entry says nothing
+            strides = [tuple(0 if n == 1 else s for n, s in zip(*a)) for a in zip(shapes, strides)]
         if (set(map(_dtype, ts)) != _only_int64 or set(map(_device, ts)) != {index} or list(map(_size, ts[:n_x])) != shapes
                 or not all(map(_contiguous, ts[8:])) or numbers[0::2] != words or numbers[1::2] != words or strides[0::2] != strides[1::2]
                 or (dk > 1 and (strides[0][-1] != 1 or strides[2][-1] != 1)) or (dv > 1 and (strides[4][-1] != 1 or strides[6][-1] != 1))):

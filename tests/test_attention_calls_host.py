@@ -89,3 +89,30 @@ def test_a_call_that_grows_the_workspace_keeps_its_tensors(library, call):
     assert all(id(t) in held for t in tensors)
     lane.sync()
     assert not lane._pending
+
+
+@pytest.mark.parametrize("B,T,H,d", [(1, 3, 2, 4), (2, 1, 2, 4), (2, 3, 1, 4), (1, 1, 1, 4), (2, 3, 2, 1)])
+def test_the_stride_of_an_axis_of_one_entry_says_nothing(library, B, T, H, d):
+    """Both shares of q, k, v and the output lie alike, other than in what a view of one entry calls its stride."""
+    library.room = True
+    lane, decay = host_lane(), torch.zeros(H, 65, dtype=torch.int32)
+
+    def shares(*shape):
+        a, b = pair(*shape)
+        return a, b.as_strided(shape, [1 << 30 if n == 1 else s for n, s in zip(shape, b.stride())])
+    rows, tok, cell = B * H * T, B * H * T * 64, B * H * d * d
+    mat = material(mpc._ATTENTION_MASKS, a_q=rows * d, a_k=rows * d, a_qd=rows * d, a_kd=rows * d, a_v=rows * d, a_w=tok, a_s=cell, c_p=tok, c_u=cell, c_o=rows * d)
+    lane.linear_attention(shares(B, T, H, d), shares(B, T, H, d), shares(B, T, H, d), decay, mat, out=shares(B, T, H, d))
+    n = B * H
+    mat = material(mpc._STEP_MASKS, a_q=n * d, a_k=n * d, a_v=n * d, a_s=cell, c_u=cell, c_o=n * d)
+    lane.linear_attention_step(shares(B, H, d), shares(B, H, d), shares(B, H, d), decay, mat, pair(B, H, d, d), out=shares(B, H, d))
+    assert [name for name, _ in library.calls] == ["mpc_linear_attention", "mpc_linear_attention_step"]
+
+
+def test_shares_that_lie_differently_are_refused(library):
+    lane, (a, b) = host_lane(), pair(2, 2, 4)
+    n, cell = 4, 2 * 2 * 16
+    mat = material(mpc._STEP_MASKS, a_q=n * 4, a_k=n * 4, a_v=n * 4, a_s=cell, c_u=cell, c_o=n * 4)
+    with pytest.raises(ValueError):
+        lane.linear_attention_step((a, b.transpose(0, 1)), pair(2, 2, 4), pair(2, 2, 4), torch.zeros(2, 65, dtype=torch.int32), mat, pair(2, 2, 4, 4))
+    assert not library.calls

@@ -72,3 +72,9 @@ def test_strides_whose_extent_wraps_are_refused(tmp_path):
     r = fake_hip.run(tmp_path, REFUSALS + "launches()\n" + STRIDES)
     assert r["prompt"] == [R] * 6 and r["step"] == [R] * 2 and r["launched by refused calls"] == []
     assert r["one"] == [0] * 2
+
+
+def test_one_token_has_no_use_for_its_stride(tmp_path):
+    """A view of one token of a long array may have any stride there; with two tokens the limit holds."""
+    r = fake_hip.run(tmp_path, REFUSALS + "result['one'] = [prompt(T=t, sq=Strides(H * dk, 1 << 23, dk)) for t in (1, 2)]")
+    assert r["one"] == [0, R]
