@@ -100,6 +100,9 @@ def scores_backward(lane: "mpc.Lane", go, q, k, v, scores, buckets, n_buckets, t
 
 
 # ------------------------------------------------------------------------------------------------ prompts and single tokens
+_ROWS = 16384                     # of a projection at a time
+
+
 @dataclasses.dataclass
 class TokenLayer:
     """Attention layer with public 4-bit projections: x -> [q | k | v] -> linear attention -> out projection."""
@@ -114,15 +117,27 @@ class TokenLayer:
     decay: torch.Tensor            # [heads, 65]
     scale_bits: int = 20
 
+    def _product(self, lane, x, w, scales):
+        """x [M, K] by one projection, in blocks of rows: the call takes 65535, and its workspace has up to 4 KB for each row and
+        256 columns."""
+        M = x[0].shape[0]
+        if M <= _ROWS:
+            return lane.matvec4(x, w, scales, self.group, self.scale_bits)
+        out = tuple(torch.empty((M, w.shape[0]), dtype=torch.int64, device=x[0].device) for _ in range(2))
+        for r in range(0, M, _ROWS):
+            rows = lambda s: tuple(t[r:r + _ROWS] for t in s)
+            lane.matvec4(rows(x), w, scales, self.group, self.scale_bits, out=rows(out))
+        return out
+
     def _project(self, lane, x, shape):
         """x [M, width] -> q, k, v as views [*shape, heads, d] of one product"""
-        qkv = lane.matvec4(x, self.w_qkv, self.s_qkv, self.group, self.scale_bits)
+        qkv = self._product(lane, x, self.w_qkv, self.s_qkv)
         nk = self.heads * self.dk
         part = lambda a, b, d: tuple(t[:, a:b].unflatten(0, shape).unflatten(-1, (self.heads, d)) for t in qkv)
         return part(0, nk, self.dk), part(nk, 2 * nk, self.dk), part(2 * nk, 2 * nk + self.heads * self.dv, self.dv)
 
     def _out(self, lane, o, rows):
-        return lane.matvec4(tuple(t.view(rows, -1) for t in o), self.w_out, self.s_out, self.group, self.scale_bits)
+        return self._product(lane, tuple(t.view(rows, -1) for t in o), self.w_out, self.s_out)
 
     def prompt(self, lane: "mpc.Lane", x, mat, state=None):
         """x [B, T, width] sharing -> (y [B, T, rows of w_out], state after the last token)"""
