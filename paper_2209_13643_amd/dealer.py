@@ -129,8 +129,8 @@ def _folded_addend(lane: "mpc.Lane", g, products):
 
 def _ring_product(lane: "mpc.Lane", A, B):
     """Batched ring product over all leading axes, waited for; the call takes 32767 matrices."""
+    left, right = A.reshape((-1,) + tuple(A.shape[-2:])), B.reshape((-1,) + tuple(B.shape[-2:]))     # may copy: ahead of the wait
     lane.wait_torch()
-    left, right = A.reshape((-1,) + tuple(A.shape[-2:])), B.reshape((-1,) + tuple(B.shape[-2:]))
     Z = [lane.ring_matmul(left[n:n + 32767], right[n:n + 32767]) for n in range(0, left.shape[0], 32767)]
     lane.sync()
     return (Z[0] if len(Z) == 1 else torch.cat(Z)).view(tuple(A.shape[:-1]) + (B.shape[-1],))

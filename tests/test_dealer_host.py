@@ -26,3 +26,22 @@ def test_ring_products_of_any_number_of_matrices(lead):
     a, b = (torch.randint(-1 << 62, 1 << 62, (*lead, *s), generator=g) for s in ((2, 3), (3, 1)))
     z = dealer._ring_product(Plain(), a, b)
     assert z.shape == (*lead, 2, 1) and torch.equal(z, a @ b)
+
+
+def test_copies_of_the_operands_are_waited_for():
+    """Operands that are not dense are copied by torch: the lane waits for it behind that."""
+    order = []
+
+    class Watched(Plain):
+        def wait_torch(self):
+            order.append("wait")
+
+    class Strided(torch.Tensor):
+        @classmethod
+        def __torch_function__(cls, func, types, args=(), kwargs=None):
+            if func is torch.Tensor.reshape:
+                order.append("copy")
+            return super().__torch_function__(func, types, args, kwargs or {})
+    a = torch.arange(12).view(2, 3, 2).transpose(1, 2).as_subclass(Strided)
+    dealer._ring_product(Watched(), a, a.transpose(1, 2))
+    assert order.index("wait") > max(i for i, o in enumerate(order) if o == "copy")
