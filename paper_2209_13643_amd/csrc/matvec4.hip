@@ -90,6 +90,13 @@ template <int G> __global__ __launch_bounds__(256) void k_digits4(MatvecArgs q)
     }
 }
 
+// What lanes of a wave hand to one another through LDS: the hardware has a wave's accesses in order, and the compiler keeps them so.
+__device__ __forceinline__ void wave_in_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // A workgroup has 16 rows of the weights and MT rows of x; its waves share the columns, a block at a time.  MADE: the digits are
 // in memory, else a wave makes those of its blocks.
 template <int G, int MT, bool MADE>
@@ -155,7 +162,7 @@ __global__ __launch_bounds__(64 * most_waves(MT)) void k_matvec4(MatvecArgs q)
 #pragma unroll
                     for (int p = 0; p < 8; ++p) mine[D::at(party, g8, odd) + p * D::dwords] = d[p];
                 }
-                __builtin_amdgcn_wave_barrier();                        // one wave: its LDS accesses are in order
+                wave_in_order();
             }
 #pragma unroll
             for (int s = 0; s < D::sets; ++s) {
@@ -182,6 +189,7 @@ __global__ __launch_bounds__(64 * most_waves(MT)) void k_matvec4(MatvecArgs q)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) z[m][r] += (int64_t)(acc[r] >> 4) * scale[s][r];   // the sixteenth is exact
             }
+            if constexpr (!MADE) wave_in_order();                       // read, before the next row's or block's are written
             if (MT > 1) __builtin_amdgcn_sched_barrier(0);
         }
     }
