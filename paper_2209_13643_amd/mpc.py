@@ -340,10 +340,11 @@ def _pairs(*sharings):
     return out
 
 
-def _int32(*sizes):
-    """Sizes as the library takes them; ctypes would cut off what is beyond."""
-    if max(sizes) > 0x7FFFFFFF:
-        raise ValueError(f"sizes below 2^31 expected, got {sizes}")
+_INT = 0x7FFFFFFF            # the library's sizes; ctypes would cut off what is beyond
+
+
+def _beyond_int(*sizes):
+    raise ValueError(f"sizes below 2^31 expected, got {sizes}")
 
 
 def _words(tensors, shapes, index, names):
@@ -1001,7 +1002,8 @@ class Lane:
         shape = scores[0].shape
         B, H, Tq, Tk = shape
         n = table[0].shape[0]
-        _int32(*shape, n)
+        if max(shape) > _INT or n > _INT:
+            _beyond_int(*shape, n)
         out = out if out is not None else (torch.empty_like(scores[0]), torch.empty_like(scores[1]))
         ts, small = _pairs(("scores", scores), ("table", table), ("out", out)), (n, H)
         at = _words(ts, [shape, shape, small, small, shape, shape], self._index, ("scores", "table", "out"))
@@ -1016,7 +1018,8 @@ class Lane:
         zeros at masked pairs; it is written to scores_out (may be g), or not at all if that is None."""
         shape = g[0].shape
         B, H, Tq, Tk = shape
-        _int32(*shape, n_buckets)
+        if max(shape) > _INT or n_buckets > _INT:
+            _beyond_int(*shape, n_buckets)
         if out is None:
             out = tuple(torch.empty((n_buckets, H), dtype=torch.int64, device=self.device) for _ in range(2))
         ts, small = _pairs(("g", g), ("out", out), ("scores_out", scores_out if scores_out is not None else g)), (n_buckets, H)
@@ -1034,7 +1037,8 @@ class Lane:
         shape = x[0].shape
         M, K = shape
         N = w.shape[0]
-        _int32(M, K, N, group)
+        if M > _INT or K > _INT or N > _INT or group > _INT:
+            _beyond_int(M, K, N, group)
         out = out if out is not None else tuple(torch.empty((M, N), dtype=torch.int64, device=self.device) for _ in range(2))
         if group <= 0:
             raise ValueError(f"group: a positive number of columns expected, got {group}")
@@ -1071,7 +1075,8 @@ class Lane:
     def _attend(self, q, k, v, decay, mat, state, out, state_out, lead, dk, dv, masks, words):
         B, H, index, L, prompt = lead[0], lead[-1], self._index, lib(), len(lead) == 3
         cell = (B, H, dk, dv)
-        _int32(*lead, dk, dv)
+        if max(lead) > _INT or dk > _INT or dv > _INT:
+            _beyond_int(*lead, dk, dv)
         out = out if out is not None else tuple(torch.empty((*lead, dv), dtype=torch.int64, device=self.device) for _ in range(2))
         state_out = state_out if state_out is not None else tuple(torch.empty(cell, dtype=torch.int64, device=self.device) for _ in range(2))
         row, col = (*lead, dk), (*lead, dv)
