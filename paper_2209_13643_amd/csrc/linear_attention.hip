@@ -110,55 +110,50 @@ template <bool ADJACENT, bool PAIRS = true> struct Tile {
     }
 };
 
-// A thread's quads of an operand: load(i) asks for words, form(i, words, own0, open, mask1) makes party 0's operand x_0 + e_1, the
-// opened words and party 1's mask of them.  All words are asked for at once, ahead of the barrier behind which the last products'
-// operands may be written over: one after the other their latency was most of a job's time.
-template <bool LEFT, class T, class Load, class Form> __device__ __forceinline__ void bring(u8* lds, const T& t, Load load, Form form)
+// A thread's four quads of an operand.  Their words are asked for together, ahead of the barrier behind which the last products'
+// operands may be written over: one after the other their latency was most of a job's time.  The barrier stands outside of what
+// only one half of the waves does.
+//
+// Words of a sharing and of its mask.
+struct Masked { Quad x0, x1, a0, a1; };
+struct Words { const u64 *x0, *x1; long long stride; const u64 *a0, *a1; long long a_stride; };
+template <class T> __device__ __forceinline__ Masked masked(const T& t, const Words& w, int i)
 {
-    const decltype(load(0)) words[4] = { load(0), load(1), load(2), load(3) };
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        Quad own, open, mask;
-        form(i, words[i], own, open, mask);
-        t.stage(lds, LEFT ? kOwnLeft : kOwnRight, i, own);
-        t.stage(lds, LEFT ? kOpenLeft : kOpenRight, i, open);
-        if (!LEFT) t.stage(lds, kMaskRight, i, mask);
-    }
+    return Masked{ t.load(w.x0, w.stride, i), t.load(w.x1, w.stride, i), t.load(w.a0, w.a_stride, i), t.load(w.a1, w.a_stride, i) };
 }
-
-// Words of a sharing and of its mask, with the public factor of each word.
-struct Masked { Quad x0, x1, a0, a1; uint32_t f[4]; };
-template <bool DECAY> __device__ __forceinline__ void open_quad(const Masked& r, int bits, Quad& own, Quad& open, Quad& e0, Quad& e1)
+// party 0's operand x_0 + e_1 and the opened words; DECAY: of words times public factors f(j), rescaled
+struct NoPower { __device__ uint32_t operator()(int) const { return 1; } };
+template <bool DECAY, class Power> __device__ __forceinline__ void open_quad(const Masked& r, Power f, int bits, Quad& own, Quad& open, Quad& e0, Quad& e1)
 {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         u64 w0 = r.x0.w[j], w1 = r.x1.w[j];
-        if (DECAY) { w0 = rescaled<0>(w0 * r.f[j], bits); w1 = rescaled<1>(w1 * r.f[j], bits); }
+        if (DECAY) { w0 = rescaled<0>(w0 * f(j), bits); w1 = rescaled<1>(w1 * f(j), bits); }
         e0.w[j] = w0 - r.a0.w[j]; e1.w[j] = w1 - r.a1.w[j];
         own.w[j] = w0 + e1.w[j]; open.w[j] = e0.w[j] + e1.w[j];
     }
 }
-// A masked operand: a word's power(i, j) is a public factor, followed by the rescale (DECAY); sent(to party 0, to party 1).
-template <bool LEFT, bool DECAY, class T, class Power, class Sent>
-__device__ __forceinline__ void bring_masked(u8* lds, const T& t, const u64* x0, const u64* x1, long long stride,
-                                             const u64* a0, const u64* a1, long long a_stride, Power power, int bits, Sent sent)
+// party 0's operand, the opened words and, of a right operand, party 1's mask
+template <bool LEFT, class T> __device__ __forceinline__ void stage_operand(u8* lds, const T& t, int i, Quad own, Quad open, Quad mask)
 {
-    bring<LEFT>(lds, t, [&](int i) {
-            Masked r{ t.load(x0, stride, i), t.load(x1, stride, i), t.load(a0, a_stride, i), t.load(a1, a_stride, i), {} };
-            if (DECAY)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) r.f[j] = power(i, j);
-            return r;
-        },
-        [&](int i, const Masked& r, Quad& own, Quad& open, Quad& mask) {
-            Quad e0, e1;
-            open_quad<DECAY>(r, bits, own, open, e0, e1);
-            mask = r.a1;
-            sent(e1, e0);
-            t.clear(i, own); t.clear(i, open); t.clear(i, mask);
-        });
+    t.clear(i, own); t.clear(i, open);
+    t.stage(lds, LEFT ? kOwnLeft : kOwnRight, i, own);
+    t.stage(lds, LEFT ? kOpenLeft : kOpenRight, i, open);
+    if (!LEFT) { t.clear(i, mask); t.stage(lds, kMaskRight, i, mask); }
 }
+// power(i, j): the public factor of word j of quad i; sent(to party 0, to party 1)
+template <bool LEFT, bool DECAY, class T, class Power, class Sent>
+__device__ __forceinline__ void stage_masked(u8* lds, const T& t, const Masked (&w)[4], Power power, int bits, Sent sent)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        Quad own, open, e0, e1;
+        open_quad<DECAY>(w[i], [&](int j) { return power(i, j); }, bits, own, open, e0, e1);
+        sent(e1, e0);
+        stage_operand<LEFT>(lds, t, i, own, open, w[i].a1);
+    }
+}
+struct NoPowers { __device__ uint32_t operator()(int, int) const { return 1; } };
 
 // The receive buffers of a workgroup hold what a thread sends at a time, a quad in either direction: they stay in the L2 (with room
 // for a whole tile, 128 KB a workgroup, they were written back to memory, 160 MB a launch of 8 x 512 tokens of 12 heads).
@@ -269,8 +264,6 @@ struct Jobs {
     __device__ __forceinline__ void next() { n += step; }
 };
 
-struct NoPower { __device__ uint32_t operator()(int, int) const { return 1; } };
-
 // P, W and W V of a chunk, or one tile of its U.  8 x 512 tokens of 12 heads of 64 x 64: 218 us of the call's 294, 0.71 GB.  Bound by
 // what follows one another in a product: its loads (3.3 TB/s over all), the digits (vector instructions fill 23 % of the cycles)
 // and the matrix instructions (14 %), since five operand tiles leave room for one workgroup to a compute unit.
@@ -310,8 +303,12 @@ __global__ __launch_bounds__(kThreads) void k_chunk_open(ChunkArgs q)
                 const Place ps = anew(p);
                 const Tile<true> t(ps, L, q.dk - k0);
                 const long long oa = at * q.dk + k0;
-                if (left) bring_masked<true, false>(lds, t, q.k.p[0] + ok + k0, q.k.p[1] + ok + k0, q.k.t, q.a_k[0] + oa, q.a_k[1] + oa, q.dk, NoPower{}, 0, to_box);
-                else bring_masked<false, false>(lds, t, q.q.p[0] + oq + k0, q.q.p[1] + oq + k0, q.q.t, q.a_q[0] + oa, q.a_q[1] + oa, q.dk, NoPower{}, 0, to_box);
+                const Words from = left ? Words{ q.k.p[0] + ok + k0, q.k.p[1] + ok + k0, q.k.t, q.a_k[0] + oa, q.a_k[1] + oa, q.dk }
+                                        : Words{ q.q.p[0] + oq + k0, q.q.p[1] + oq + k0, q.q.t, q.a_q[0] + oa, q.a_q[1] + oa, q.dk };
+                const Masked w[4] = { masked(t, from, 0), masked(t, from, 1), masked(t, from, 2), masked(t, from, 3) };
+                __syncthreads();
+                if (left) stage_masked<true, false>(lds, t, w, NoPowers{}, 0, to_box);
+                else stage_masked<false, false>(lds, t, w, NoPowers{}, 0, to_box);
                 multiply_all(lds, ps, t, q.a_k[1] + oa, q.dk, z0, z1);
             }
             Quad own[2], open[2], mask[2];                        // W
@@ -337,9 +334,7 @@ __global__ __launch_bounds__(kThreads) void k_chunk_open(ChunkArgs q)
                 const int first = ps.wave / 4 * 2;                // all waves bring V, two quads each
                 Masked v[2];
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    v[i] = Masked{ tv.load(q.v.p[0] + o, q.v.t, first + i), tv.load(q.v.p[1] + o, q.v.t, first + i),
-                                   tv.load(q.a_v[0] + oa, q.dv, first + i), tv.load(q.a_v[1] + oa, q.dv, first + i), {} };
+                for (int i = 0; i < 2; ++i) v[i] = masked(tv, Words{ q.v.p[0] + o, q.v.p[1] + o, q.v.t, q.a_v[0] + oa, q.a_v[1] + oa, q.dv }, first + i);
                 each_word(ps, [&](int r, int i, int j) {
                     const unsigned at_o = min(i, L - 1) * q.dv + min(j, q.dv - n0 - 1);
                     z0[r] = (q.c_o[0] + oa)[at_o]; z1[r] = (q.c_o[1] + oa)[at_o];
@@ -349,7 +344,7 @@ __global__ __launch_bounds__(kThreads) void k_chunk_open(ChunkArgs q)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     Quad vo, vp, e0, e1;
-                    open_quad<false>(v[i], 0, vo, vp, e0, e1);    // sent with U's tiles
+                    open_quad<false>(v[i], NoPower{}, 0, vo, vp, e0, e1);    // sent with U's tiles
                     tv.clear(first + i, vo); tv.clear(first + i, vp); tv.clear(first + i, v[i].a1);
                     tv.stage(lds, kOwnRight, first + i, vo); tv.stage(lds, kOpenRight, first + i, vp); tv.stage(lds, kMaskRight, first + i, v[i].a1);
                     stage_at(w_at + kOwnLeft * kOperand + i * 256, own[i]);
@@ -368,13 +363,18 @@ __global__ __launch_bounds__(kThreads) void k_chunk_open(ChunkArgs q)
                 const unsigned o = min(m0 + i, q.dk - 1) * q.dv + min(n0 + j, q.dv - 1);
                 z0[r] = (q.c_u[0] + cell)[o]; z1[r] = (q.c_u[1] + cell)[o];
             });
-            const Tile<false, false> tk(p, q.dk - m0, L), tv(p, q.dv - n0, L);
+            const Tile<false, false> tk(p, q.dk - m0, L);
             const long long oa = at * q.dk + m0, oav = at * q.dv + n0;
-            if (left) bring_masked<true, true>(lds, tk, q.k.p[0] + ok + m0, q.k.p[1] + ok + m0, q.k.t, q.a_kd[0] + oa, q.a_kd[1] + oa, q.dk,
-                    [&](int, int j) { return pow[max(L - 1 - tk.k(j), 0)]; }, q.bits,
-                    [&](const Quad& e1, const Quad& e0) { if (n0 == 0) box.put(e1, e0); });
-            else bring_masked<false, false>(lds, tv, q.v.p[0] + ov + n0, q.v.p[1] + ov + n0, q.v.t, q.a_v[0] + oav, q.a_v[1] + oav, q.dv, NoPower{}, 0,
-                    [&](const Quad& e1, const Quad& e0) { if (m0 == 0) box.put(e1, e0); });
+            const Words from = left ? Words{ q.k.p[0] + ok + m0, q.k.p[1] + ok + m0, q.k.t, q.a_kd[0] + oa, q.a_kd[1] + oa, q.dk }
+                                    : Words{ q.v.p[0] + ov + n0, q.v.p[1] + ov + n0, q.v.t, q.a_v[0] + oav, q.a_v[1] + oav, q.dv };
+            const Tile<false, false> t(p, left ? q.dk - m0 : q.dv - n0, L);
+            const Masked w[4] = { masked(t, from, 0), masked(t, from, 1), masked(t, from, 2), masked(t, from, 3) };
+            uint32_t f[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f[j] = pow[max(L - 1 - t.k(j), 0)];
+            __syncthreads();
+            if (left) stage_masked<true, true>(lds, t, w, [&](int, int j) { return f[j]; }, q.bits, [&](const Quad& e1, const Quad& e0) { if (n0 == 0) box.put(e1, e0); });
+            else stage_masked<false, false>(lds, t, w, NoPowers{}, 0, [&](const Quad& e1, const Quad& e0) { if (m0 == 0) box.put(e1, e0); });
             multiply_all(lds, p, tk, q.a_kd[1] + oa, q.dk, z0, z1);
             each_word(anew(p), [&](int r, int i, int j) {
                 const int d = m0 + i, e = n0 + j;
@@ -417,7 +417,6 @@ __global__ __launch_bounds__(kThreads) void k_chunk_out(ChunkArgs q)
     const Place at_start = place();
     const bool left = at_start.wave < 4;
     const Box box(q.box);
-    struct Three { Quad own, open, mask; };
     for (Jobs job(q.cells, q.nt); job.cell() < q.cells; job.next()) {
         const Place p = anew(at_start);
         const int n0 = job.kind() * 64, bh = job.cell() / q.chunks, chunk = job.cell() - bh * q.chunks;
@@ -433,20 +432,24 @@ __global__ __launch_bounds__(kThreads) void k_chunk_out(ChunkArgs q)
             const Place ps = anew(p);
             const Tile<true> tq(ps, L, q.dk - k0);
             const long long oa = at * q.dk + k0;
+            const Tile<false> ts(ps, q.dv - n0, q.dk - k0);
+            Masked w[4];                                              // of the state: party 0's operand, the opened words and party 1's mask
+            uint32_t f[4];
             if (left) {
                 const long long o = b * q.q.b + h * q.q.h + t0 * q.q.t + k0;
-                bring_masked<true, true>(lds, tq, q.q.p[0] + o, q.q.p[1] + o, q.q.t, q.a_qd[0] + oa, q.a_qd[1] + oa, q.dk,
-                    [&](int i, int) { return pow[min(tq.row(i), L - 1) + 1]; }, q.bits,
-                    [&](const Quad& e1, const Quad& e0) { if (n0 == 0) box.put(e1, e0); });
+                const Words from{ q.q.p[0] + o, q.q.p[1] + o, q.q.t, q.a_qd[0] + oa, q.a_qd[1] + oa, q.dk };
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { w[i] = masked(tq, from, i); f[i] = pow[min(tq.row(i), L - 1) + 1]; }
             } else {
                 const long long o = ((long long)job.cell() * q.dk + k0) * q.dv + n0;
-                const Tile<false> t(ps, q.dv - n0, q.dk - k0);
-                bring<false>(lds, t, [&](int i) { return Three{ t.load(q.u[0] + o, q.dv, i), t.load(q.u[1] + o, q.dv, i), t.load(q.a_s[1] + o, q.dv, i) }; },
-                    [&](int i, const Three& r, Quad& own, Quad& open, Quad& mask) {
-                        own = r.own; open = r.open; mask = r.mask;
-                        t.clear(i, own); t.clear(i, open); t.clear(i, mask);
-                    });
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { w[i].x0 = ts.load(q.u[0] + o, q.dv, i); w[i].x1 = ts.load(q.u[1] + o, q.dv, i); w[i].a1 = ts.load(q.a_s[1] + o, q.dv, i); }
             }
+            __syncthreads();
+            if (left) stage_masked<true, true>(lds, tq, w, [&](int i, int) { return f[i]; }, q.bits, [&](const Quad& e1, const Quad& e0) { if (n0 == 0) box.put(e1, e0); });
+            else
+#pragma unroll
+                for (int i = 0; i < 4; ++i) stage_operand<false>(lds, ts, i, w[i].x0, w[i].x1, w[i].a1);
             multiply_all(lds, ps, tq, q.a_qd[1] + oa, q.dk, z0, z1);
         }
         const long long to = b * q.ob + h * q.oh + t0 * q.ot + n0;
