@@ -41,13 +41,15 @@ def relative_buckets(Tq: int, Tk: int, n_buckets: int, max_distance: int, causal
 
 
 def decay_powers(decay, frac_bits: int = 16) -> torch.Tensor:
-    """Powers 0..64 of every head's decay in [0, 1] as fixed point, int32 [H, 65]."""
-    d = torch.as_tensor(decay, dtype=torch.float64)
+    """Powers 0..64 of every head's decay in [0, 1] as fixed point, int32 [H, 65], on the device of a tensor; formed on the host,
+    where all devices' tables are the same."""
+    given = torch.as_tensor(decay, dtype=torch.float64)
+    d = given.cpu()
     if d.ndim != 1 or not bool(((d >= 0) & (d <= 1)).all()):
         raise ValueError("one decay in [0, 1] for each head expected")
     if not 0 <= frac_bits <= 30:
         raise ValueError("frac_bits in [0, 30] expected: a decay of one has to fit 31 bits")
-    return torch.round(d[:, None] ** torch.arange(mpc.ATTENTION_CHUNK + 1) * 2.0 ** frac_bits).to(torch.int32)
+    return torch.round(d[:, None] ** torch.arange(mpc.ATTENTION_CHUNK + 1) * 2.0 ** frac_bits).to(torch.int32).to(given.device)
 
 
 def pack_weights4(q: torch.Tensor) -> torch.Tensor:

@@ -165,3 +165,9 @@ def test_matvec4_one_group_for_all_columns(mpc, lane, attention):  # noqa: F811
     z = lane.matvec4(dev(mpc, x), attention.pack_weights4(torch.from_numpy(q)).cuda(), mpc.to_device(s), (1 << 31) - 128, 20)
     lane.sync()
     equal(mpc, z, plain.matvec4(x, q, s, 384, 20))
+
+
+def test_decays_that_lie_on_the_device(mpc, attention):  # noqa: F811
+    d = torch.tensor([0.0, 0.97, 1 - 2.0 ** -7, 1.0], dtype=torch.float64)
+    on_device = attention.decay_powers(d.cuda(), 20)
+    assert on_device.is_cuda and torch.equal(on_device.cpu(), attention.decay_powers(d, 20))
