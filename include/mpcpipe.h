@@ -519,9 +519,12 @@ int mpc_maxpool2x2_backward(mpc_ctx* ctx, mpc_cshare g, mpc_cshare s1, mpc_cshar
 
 /* The encoder layer's attention is linear here: scores feed the second product directly (Sec. 5.3's products, the softmax
  * left out).  The calls below give it positions, a form whose cost grows with the length instead of its square and that
- * serves single tokens, and projections by public weights.  They run on the lane's first stream, on every lane, and their
- * exchanges are remote stores whatever mpc_ctx_set_exchange says.  Outputs may not overlap an input other than where it is
- * said (MPC_EINVAL). */
+ * serves single tokens, and projections by public weights.  They run on the lane's first stream, on every lane.  Outputs may
+ * not overlap an input other than where it is said (MPC_EINVAL).
+ * The position bias and the public products are local.  The linear attention calls compute the words of Alg. 1, but do not
+ * exchange as the other calls do, whatever mpc_ctx_set_exchange says: a thread has both parties' shares of a word, forms the
+ * opened word from them and uses it at once, and work that needs the same word elsewhere forms it again.  Every masked word
+ * is stored once, where the peer's receive buffer would be (the traffic of sending it); nothing reads those buffers. */
 
 /* Learned relative position bias.  scores, out: [B][H][Tq][Tk]; table: [n_buckets][H]; buckets: public int32
  * [Tq + Tk - 1] on the device, entry j - i + Tq - 1 is the bucket of query i and key j.

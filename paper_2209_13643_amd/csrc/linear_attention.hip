@@ -11,8 +11,10 @@
 // (element by element), and the states' part of O.
 //
 // All products are Alg. 1 with party 0's local product folded into its addend (the folded calls of the linear layers):
-// party 0 has c_0 + (x_0 + e_1)(y_0 + f_1), party 1 has c_1 + e b_1 + a_1 f.  The exchange is by remote store: a masked word is
-// stored into the peer's receive buffer and used as it passes.
+// party 0 has c_0 + (x_0 + e_1)(y_0 + f_1), party 1 has c_1 + e b_1 + a_1 f.  A thread has both
+// parties' shares and forms the opened words from them, in every job that needs them; no job waits for another's.  So there is no
+// receiver.  A masked word is stored once in a call, by the job named at the store, where the peer's receive buffer would be: the
+// traffic of sending it.  Nothing reads these buffers.
 #include "attention.h"
 #include "digits.h"
 
@@ -20,7 +22,7 @@ namespace {
 
 constexpr int kChunk = MPC_ATTENTION_CHUNK;   // 64
 constexpr int kThreads = 512;
-constexpr int kBoxes = 256;                   // workgroups of a launch, one to a compute unit, each with receive buffers of its own
+constexpr int kBoxes = 256;                   // workgroups of a launch, one to a compute unit, each with send buffers of its own
 constexpr int kStateBoxes = 2048;             // workgroups of the states' launch, eight to a compute unit: 512 words each
 constexpr long long kMaxStride = MPC_ATTENTION_MAX_TOKEN_STRIDE;   // 64 tokens stay below 2^31 bytes
 constexpr size_t kBoxWords = (size_t)kThreads * 4;   // per direction
@@ -155,8 +157,8 @@ __device__ __forceinline__ void stage_masked(u8* lds, const T& t, const Masked (
 }
 struct NoPowers { __device__ uint32_t operator()(int, int) const { return 1; } };
 
-// The receive buffers of a workgroup hold what a thread sends at a time, a quad in either direction: they stay in the L2 (with room
-// for a whole tile, 128 KB a workgroup, they were written back to memory, 160 MB a launch of 8 x 512 tokens of 12 heads).
+// The send buffers of a workgroup (sent is sent: nothing reads them) hold what a thread sends at a time, a quad in either direction:
+// they stay in the L2 (with room for a whole tile, 128 KB a workgroup, they were written back to memory, 160 MB a launch of 8 x 512 tokens of 12 heads).
 struct Box {
     u64 *to0, *to1;
     __device__ __forceinline__ Box(u64* box) : to0(box + blockIdx.x * 2 * kBoxWords + threadIdx.x * 2), to1(to0 + kBoxWords) {}
@@ -476,8 +478,8 @@ constexpr int kSlice = 32;                    // columns of the state in a workg
 constexpr int kGroups = 256 / (kSlice / 2);   // rows at a time
 constexpr int kStepBoxes = 1024;              // four workgroups to a compute unit
 constexpr int kMaxD = MPC_ATTENTION_MAX_D;
-// receive buffers of a workgroup, per direction: k and q, v, and the two rows of the state that a thread sends at a time; they stay
-// in the L2
+// send buffers of a workgroup, per direction: k and q, v, and the two rows of the state that a thread sends at a time; they stay in
+// the L2
 constexpr size_t kStepBoxWords = 2 * kMaxD + kSlice + 2 * 256 * 2;
 
 struct StepShared {
@@ -559,7 +561,7 @@ template <bool WHOLE> __device__ __forceinline__ void step_slice(const StepArgs&
 }
 
 // A state element moves 64 bytes (the state, its mask and the outer product's addend of both parties in, the new state out): bound
-// by HBM.  2048 heads of 64 x 64: 110 us, 5.1 TB/s; with slices of 16 columns 124, with ordinary stores 118, with receive buffers
+// by HBM.  2048 heads of 64 x 64: 110 us, 5.1 TB/s; with slices of 16 columns 124, with ordinary stores 118, with send buffers
 // for a whole slice, which leave the L2, 139.
 __global__ __launch_bounds__(256, 4) void k_step(StepArgs q)
 {
