@@ -549,8 +549,9 @@ int mpc_position_bias_grad(mpc_ctx* ctx, mpc_cshare g, const int32_t* buckets, m
  * odd k in its high half, in two's complement (what lies behind column K is not used).  scales: int32
  * [N][ceil(K / group)] with scale_bits fraction bits in [0, 31]; the product is rescaled by them (the local truncation of
  * mpc_truncate), so z has the fixed point of x.  group: 32, 64 or a multiple of 128.  Linear in the shares with public
- * factors, so each party works alone: no triple, no exchange.  Workspace: the query (nothing for small products).  A call reads
- * the weights once for every eight rows of x, small products once for every two or four.  MPC_ERANGE: K > MPC_MAX_K_TOTAL, M > 65535,
+ * factors, so each party works alone: no triple, no exchange.  Workspace: the query (nothing unless the digits of x are made once, in
+ * memory, or the columns are split over workgroups).  A call reads the weights once for every eight rows of x, small products
+ * once for every one, two or four.  MPC_ERANGE: K > MPC_MAX_K_TOTAL, M > 65535,
  * N > 2^25. */
 size_t mpc_matvec4_workspace_bytes(int M, int K, int N);
 int mpc_matvec4(mpc_ctx* ctx, mpc_cshare x, const uint8_t* w, const int32_t* scales, mpc_share z,

@@ -63,7 +63,7 @@ def pack_weights4(q: torch.Tensor) -> torch.Tensor:
 
 def quantize4(w: torch.Tensor, group: int, scale_bits: int = 20):
     """Nearest 4-bit form of real weights [N, K]: (packed weights, int32 scales [N, ceil(K / group)]); a group's scale is its
-    largest magnitude over 7."""
+    largest magnitude over 7.  The product takes the same scale_bits (Lane.matvec4's own default is 16)."""
     N, K = w.shape
     if group <= 0 or not bool((w.abs().double() * 2.0 ** scale_bits / 7 < 2 ** 31 - 1).all()):
         raise ValueError("a positive group and finite weights whose scales fit 31 bits expected")
@@ -107,7 +107,8 @@ _ROWS = 16384                     # of a projection at a time
 
 @dataclasses.dataclass
 class TokenLayer:
-    """Attention layer with public 4-bit projections: x -> [q | k | v] -> linear attention -> out projection."""
+    """Attention layer with public 4-bit projections: x -> [q | k | v] -> linear attention -> out projection.  Results are new
+    tensors: a graph is recorded of the lane's calls with out arguments instead."""
     heads: int
     dk: int
     dv: int

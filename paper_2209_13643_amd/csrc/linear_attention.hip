@@ -266,9 +266,11 @@ struct Jobs {
     __device__ __forceinline__ void next() { n += step; }
 };
 
-// P, W and W V of a chunk, or one tile of its U.  8 x 512 tokens of 12 heads of 64 x 64: 218 us of the call's 294, 0.71 GB.  Bound by
+// P, W and W V of a chunk, or one tile of its U.  8 x 512 tokens of 12 heads of 64 x 64: 214 us of the call's 291, 0.71 GB.  Bound by
 // what follows one another in a product: its loads (3.3 TB/s over all), the digits (vector instructions fill 23 % of the cycles)
-// and the matrix instructions (14 %), since five operand tiles leave room for one workgroup to a compute unit.
+// and the matrix instructions (14 %), since five operand tiles leave room for one workgroup to a compute unit.  All 256 registers
+// are used, and 19 words are spilled (80 bytes a lane): nine offsets, read again in every job, and ten words of U's jobs between
+// their loads and their digits.
 __global__ __launch_bounds__(kThreads) void k_chunk_open(ChunkArgs q)
 {
     extern __shared__ __attribute__((aligned(16))) u8 lds[];          // kOperands kOperand
@@ -389,7 +391,8 @@ __global__ __launch_bounds__(kThreads) void k_chunk_open(ChunkArgs q)
 }
 
 // From chunk to chunk, a state element to a thread: what the chunk's O needs of S takes the place of its U.  Bound by HBM, 48 bytes an
-// element and chunk: 32 us for the same 768 chunks, 4.7 TB/s.
+// element and chunk: 33 us for the same 768 chunks, 4.6 TB/s.  Few heads with many chunks are bound by latency: a chunk's words are
+// asked for only behind the stores of the one before.
 __global__ __launch_bounds__(256) void k_chunk_states(ChunkArgs q)
 {
     const long long per = (long long)q.dk * q.dv, n = (long long)q.B * q.H * per;
@@ -411,7 +414,7 @@ __global__ __launch_bounds__(256) void k_chunk_states(ChunkArgs q)
     }
 }
 
-// O of a chunk, 64 columns of dv: the states' part joins what the chunk has for itself.  72 us there, 3.8 TB/s, bound as k_chunk_open;
+// O of a chunk, 64 columns of dv: the states' part joins what the chunk has for itself.  71 us there, 3.9 TB/s, bound as k_chunk_open;
 // what is read and written for good passes by the caches (the call 301 -> 296).
 __global__ __launch_bounds__(kThreads) void k_chunk_out(ChunkArgs q)
 {
@@ -562,7 +565,9 @@ template <bool WHOLE> __device__ __forceinline__ void step_slice(const StepArgs&
 
 // A state element moves 64 bytes (the state, its mask and the outer product's addend of both parties in, the new state out): bound
 // by HBM.  2048 heads of 64 x 64: 110 us, 5.1 TB/s; with slices of 16 columns 124, with ordinary stores 118, with send buffers
-// for a whole slice, which leave the L2, 139.
+// for a whole slice, which leave the L2, 139.  96 heads of 64 x 64 are 192 workgroups, not enough for the chip's memory: 10 us, 2.6
+// TB/s.  Columns that fill no slice are moved word by word: 640 heads of 97 x 99 131 us, of 96 x 96 79.  Four workgroups to a
+// unit leave a thread 128 registers: three addresses are spilled (28 bytes a lane) and read again once a slice, none for a row.
 __global__ __launch_bounds__(256, 4) void k_step(StepArgs q)
 {
     __shared__ StepShared lds;

@@ -5,8 +5,10 @@
 // On the matrix cores the weights are the left operand, 16 rows, and a row of x is the right one: its 16 columns are the eight
 // digits of both parties' words, so one 16 x 16 x 64 product serves a whole row.  The digit sums of a group are exact in 32
 // bits, times the group's scale they are added up in 64, and the eight digits join at the end.  One row of 25088 x 4096 takes
-// 18 us (51 MB of weights, 2.9 TB/s): every workgroup also reads x, twice the bytes of its weights out of the L2, and without either
-// of the two it takes 12.  Several rows are bound by the digits' and the scales' vector instructions, few weights by latency.
+// 16 to 18 us (51 MB of weights, 2.9 to 3.2 TB/s): every workgroup also reads x, twice the bytes of its weights out of the L2, and without either
+// of the two it takes 12.  Several rows are bound by the digits' and the scales' vector instructions, few weights by latency.  Many
+// rows (a prompt's) are far from their bytes: every 16 rows of the weights read all digits of x again, 4096 x 768 x 2304 694 us for
+// 202 MB, 4096 x 768 x 768 280.
 #include "attention.h"
 #include "digits.h"
 
@@ -29,7 +31,7 @@ constexpr int kMostN = 1 << 25;               // 2^21 workgroups of up to 1024 t
 constexpr int most_waves(int mt) { return mt == 1 ? 16 : 8; }
 
 // Whether the digits of x are made once, by a launch of their own, instead of by every workgroup for itself.  us with and without:
-// 8 x 25088 x 4096 51 / 76, 16 x 4096 x 4096 33 / 44; but 4 x 4096 x 4096 12 / 12, 8 x 1024 x 4096 13 / 11, 1 x 768 x 2304 7 / 4.
+// 8 x 25088 x 4096 50 / 76, 16 x 4096 x 4096 30 / 44; but 4 x 4096 x 4096 12 / 12, 8 x 1024 x 4096 13 / 11, 1 x 768 x 2304 7 / 4.
 bool small(int M, int K, int N) { return (long long)M * K * N < 1ll << 27; }
 bool digits_in_memory(int M, int K, int N) { return M > 4 && !small(M, K, N); }
 
@@ -37,8 +39,8 @@ bool digits_in_memory(int M, int K, int N) { return M > 4 && !small(M, K, N); }
 // 4 x 768 x 768 6.7 / 4.8, but for larger products 4 x 25088 x 4096 40 / 43 and for groups of 32 4 x 4096 x 4096 15 / 20.
 int rows_at_once(int M, int K, int N) { return digits_in_memory(M, K, N) ? 8 : M < 3 ? M : 4; }
 // Into how many workgroups the columns are split: few rows of the weights that are long leave most units idle, and a workgroup's
-// waves go through several blocks one after the other.  The sums are added by a launch of their own.  us without and with:
-// 1 x 25088 x 10 31 / 11, 1 x 25088 x 1000 23 / 16, 8 x 25088 x 200 44 / 23; but for more than kUnits workgroups 1 x 25088 x 4096
+// waves go through several blocks one after the other.  The sums are added by a launch of their own.  us without and with, groups of
+// 128: 1 x 25088 x 10 14 / 8, 1 x 25088 x 1000 17 / 13, 8 x 25088 x 200 22 / 17; but for more than kUnits workgroups 1 x 25088 x 4096
 // 18 / 21, and for fewer than kLong blocks to a wave 16 x 4096 x 1000 12 / 18.
 int splits_of(int M, int K, int N)
 {
