@@ -19,7 +19,7 @@ def any_words(rng, d, shapes):
 
 
 @pytest.mark.parametrize("B,H,dk,dv", [(70, 16, 8, 33), (70, 16, 5, 64), (33, 16, 40, 70)])
-def test_steps_of_several_rounds(mpc, lane, B, H, dk, dv):  # noqa: F811
+def test_steps_of_several_jobs(mpc, lane, B, H, dk, dv):  # noqa: F811
     """More slices of 32 columns than the 1024 workgroups of a launch: k and q, partial sums and buffers are used again."""
     print(f"step {B}x{H}x{dk}x{dv}", flush=True)
     assert B * H * -(-dv // 32) > 1024
@@ -35,11 +35,11 @@ def test_steps_of_several_rounds(mpc, lane, B, H, dk, dv):  # noqa: F811
 
 # chunks x kinds of jobs beyond the 256 workgroups of a launch: kinds that take turns (2 of the first launch, 2 of the last), kinds
 # that do not (3 and 5), and more state elements than the second launch has threads (524288)
-ROUNDS = [(17, 8, 70, 16, 24), (9, 16, 10, 10, 70), (9, 8, 10, 70, 72), (5, 8, 70, 128, 128)]
+MANY = [(17, 8, 70, 16, 24), (9, 16, 10, 10, 70), (9, 8, 10, 70, 72), (5, 8, 70, 128, 128)]
 
 
-@pytest.mark.parametrize("B,H,T,dk,dv", ROUNDS)
-def test_prompts_of_several_rounds(mpc, lane, B, H, T, dk, dv):  # noqa: F811
+@pytest.mark.parametrize("B,H,T,dk,dv", MANY)
+def test_prompts_of_several_jobs(mpc, lane, B, H, T, dk, dv):  # noqa: F811
     print(f"prompt {B}x{T}x{H}x{dk}x{dv}", flush=True)
     rng = np.random.default_rng(T * dk + dv)
     cells, mt, nt = B * H * -(-T // 64), -(-dk // 64), -(-dv // 64)
